@@ -8,9 +8,9 @@ exact.  The operators, for party i (0 or 1), with t(x) the share-local rescaling
                  F[slot] = D_0 + D_1,  X_i[slot] = B_i + i F[slot]  (X_0 + X_1 is the cached value).
 ``cache_read``   rows of the cache as operands of a share product: E = F[slot], A_i = X_i[slot] - i F[slot].
 ``rotate``       rescaling of a projection, position rotation and masking of the result, in one pass.
-``scores``       queries times cached keys: t(C_i + E X_i^T + A_i F^T) - R_i for the keys a row sees.
+``scores``       queries times cached keys: t(C_i + E X_i^T + A_i F^T) - M_i for the keys a row sees.
 ``weights``      the opened masked scores squared, (s + c)^2, masked again, with the sum of every row.
-``values``       weights times cached values: t(C_i + E X_i + A_i F) - R_i.
+``values``       weights times cached values: t(C_i + E X_i + A_i F) - M_i.
 
 Masked values, shares and triple parts are uniform over the ring whatever the secrets are, so all of
 them are drawn as uniform words; tables of the rotation, lengths and pages are as a server has them.
@@ -234,7 +234,7 @@ def _prepare_rotate(case, gen):
     wide = _words(gen, t, case["fused"] * h * d)
     return dict(x_i=wide[:, :h * d], positions=torch.randint(0, longest, (t,), device="cuda", generator=gen).to(torch.int32),
                 cos=fixed(torch.cos(angle)), sin=fixed(torch.sin(angle)),
-                r_i=_words(gen, t, h * d) if case["masked"] else None,
+                m_i=_words(gen, t, h * d) if case["masked"] else None,
                 out=torch.empty(t, h * d, dtype=torch.int64, device="cuda"))
 
 
@@ -372,7 +372,7 @@ def _run_plain(s):
         y1, y2 = _rescale(x1 * c - x2 * n, party, FRAC), _rescale(x2 * c + x1 * n, party, FRAC)
         turned = torch.stack((y1, y2), -1).flatten(2) if case["interleaved"] else torch.cat((y1, y2), -1)
         y = torch.cat((turned, x[:, :, 2 * half:]), -1).view(t, h * d)
-        return y if s["r_i"] is None else y - s["r_i"]
+        return y if s["m_i"] is None else y - s["m_i"]
     token, live, seen = _layout(s)
     heads, places = case["heads"], s["max_new"]
     keys = torch.arange(s["ld"], device="cuda")
@@ -414,7 +414,7 @@ def _run_own(s):
     if op == "cache_read":
         return ctx.cache_read(party, s["f_pool"], s["x_pool"], s["slots"], out=(s["e"], s["a_i"]))
     if op == "rotate":
-        return ctx.rotate_share(party, s["x_i"], s["positions"], s["cos"], s["sin"], case["heads"], FRAC, FRAC, r_i=s["r_i"],
+        return ctx.rotate_share(party, s["x_i"], s["positions"], s["cos"], s["sin"], case["heads"], FRAC, FRAC, m_i=s["m_i"],
                                 interleaved=bool(case["interleaved"]), out=s["out"])
     if op == "weights":
         return ctx.attention_weights(party, s["batch"], s["d_0"], s["d_1"], s["r_i"], s["r2_i"], BIAS, FRAC, m_i=s["m_i"],
@@ -463,7 +463,7 @@ def exact(case, seed):
             out[:, :, lo] = scaled(c * x[:, :, lo] - n * x[:, :, hi])
             out[:, :, hi] = scaled(n * x[:, :, lo] + c * x[:, :, hi])
         out = out.reshape(out.shape[0], -1)
-        return out if s["r_i"] is None else out - s["r_i"]
+        return out if s["m_i"] is None else out - s["m_i"]
     group = case["heads"] // case["kv_heads"]
     out = torch.zeros_like(s["out"])
     sums = torch.zeros(s["t"], case["heads"], dtype=torch.int64, device="cuda")
