@@ -288,8 +288,8 @@ def prepare(case, seed):
         import paper_2505_07239_amd as comet
         s["ctx"] = comet.Context(0)
         if "q_start" in s:
-            s["batch"] = comet.KVBatch(s["q_start"], s["kv_len"], s["table"], case["page"], case["heads"], case["kv_heads"],
-                                       s["max_new"], head_mask=s["head_mask"])
+            s["batch"] = comet.KVBatch(s["t"], case["heads"], case["kv_heads"], s["q_start"], s["kv_len"], s["table"],
+                                       case["page"], s["max_new"], head_mask=s["head_mask"])
     return s
 
 
