@@ -57,7 +57,7 @@ enum {
 enum { COMET_AXIS_COLS = 0, COMET_AXIS_ROWS = 1 };
 
 /* operations known to comet_workspace_bytes() */
-enum { COMET_OP_COMPACT = 0, COMET_OP_SOMM = 1, COMET_OP_SIMM = 2 };
+enum { COMET_OP_COMPACT = 0, COMET_OP_SOMM = 1, COMET_OP_SIMM = 2, COMET_OP_SCORES = 3, COMET_OP_VALUES = 4 };
 
 /* flags of the share calls.
  * COMET_FULL_A / COMET_FULL_B: the named triple share is passed at FULL size
@@ -93,6 +93,8 @@ const char* comet_version(void);
  *   COMET_OP_COMPACT: m = n_tok, k unused, n = nb, bs unused
  *   COMET_OP_SOMM   : m, k, n = n_blk_cap * bs (compact width), bs
  *   COMET_OP_SIMM   : m, k = n_blk_cap * bs (compact contraction), n, bs
+ *   COMET_OP_SCORES : m = n_tok * n_heads, k = d, n = ld, bs unused
+ *   COMET_OP_VALUES : m = n_tok * n_heads, k = ld, n = d, bs unused
  * Returns 0 for sizes the operation would reject. */
 size_t comet_workspace_bytes(int op, int64_t m, int64_t k, int64_t n, int bs);
 
@@ -373,6 +375,120 @@ int comet_scatter_cols(comet_ctx* ctx, const uint64_t* compact, int64_t m, int b
  * two-party one.  out may alias z. */
 int comet_truncate_share(comet_ctx* ctx, int party, const uint64_t* z, uint64_t* out,
                          size_t n_elems, int frac_bits);
+
+/* ---- (6) attention over a cache of shares ------------------------------- */
+
+/* The products between the QKV and the output layer: queries with cached keys, weights with cached
+ * values (multiplications of two secrets, Eq. 1), and the local steps around them.  Lengths, pages and
+ * active heads are public, like the sparsity distribution.
+ *
+ * The cache of a key or value matrix is a pair of POOLS of rows, one row of `width` words per slot: F, the
+ * cached values masked and opened (the same on both parties), and X_i, this party's share of them,
+ *     F = X - B,      X_i = B_i + party * F,      X_0 + X_1 = X,
+ * with B the mask of the triples the cache takes part in (drawn once per cached row; every product has an A
+ * and a C = A B of its own).  With X_i in the place of B_i, Eq. 1 needs no third term:
+ *     [Z]_i = [C]_i + E [X]_i + [A]_i F                       (mod 2^64)
+ * A slot's row holds n_kv_heads times `ldp` words; the products read the first d words of a head's ldp.
+ * Keys and values may be the same pools: in latent attention a token has one row (n_kv_heads = 1) that all
+ * query heads share, all of which are keys and whose first words are values. */
+
+/* The exchanged masked shares of n_tok new rows are opened into the cache:
+ *     F[slots[t]] = d_0[t] + d_1[t],     X_i[slots[t]] = b_i[t] + party * F[slots[t]].
+ * d_0, d_1, b_i: n_tok x width; f_pool, x_pool: n_slots x width.  A token whose slot is outside the pools
+ * (-1: padding) is skipped.  No slot may occur twice in a call (which token it then holds is
+ * unspecified, and may differ from word to word).  The pools must not overlap the inputs.
+ * n_tok, width < 2^24; n_slots < 2^31. */
+int comet_cache_write(comet_ctx* ctx, int party, const uint64_t* d_0, const uint64_t* d_1,
+                      const uint64_t* b_i, const int32_t* slots, int64_t n_tok, int64_t width,
+                      uint64_t* f_pool, uint64_t* x_pool, int64_t n_slots);
+
+/* Cached rows as the activation side of a share product (a latent row expanded to keys and values by
+ * comet_somm_share, a row that moves to another cache):
+ *     e[t] = F[slots[t]],     a_i[t] = X_i[slots[t]] - party * F[slots[t]].
+ * e, a_i: n_tok x width.  The rows of a token whose slot is outside the pools are left as they were; a slot may
+ * occur any number of times.  The outputs must not overlap the pools.  Limits as for comet_cache_write. */
+int comet_cache_read(comet_ctx* ctx, int party, const uint64_t* f_pool, const uint64_t* x_pool,
+                     const int32_t* slots, int64_t n_tok, int64_t width, int64_t n_slots, uint64_t* e,
+                     uint64_t* a_i);
+
+/* Position rotation of queries or keys between their projection and their masking, in one pass.  Row t of
+ * x_i, ldx words apart, holds n_heads vectors x of head_dim words; with t(.) the share-local rescaling of
+ * comet_truncate_share,
+ *     x' = t(x by shift),      y_p = t(x'_p cos - x'_q sin by frac_bits),      y_q = t(x'_q cos + x'_p sin by frac_bits)
+ * for the pairs (p, q) = (j, j + rot_dim / 2), or (2 j, 2 j + 1) when `interleaved`, j < rot_dim / 2, with
+ * cos_t, sin_t (n_pos x rot_dim / 2 words, 2^frac_bits times the real numbers) at row positions[t], column j;
+ * the words at or beyond rot_dim are only rescaled.  out (n_tok x n_heads * head_dim) = y - m_i, the masked share
+ * that is sent to the other party; m_i may be NULL (out = y).
+ * A position outside the table is read as 0.  rot_dim: even, 0 <= rot_dim <= head_dim (0: no table).  x_i may be
+ * a column range of a wider matrix (8-byte alignment suffices for it).  out may be m_i, and must not overlap x_i.
+ * 0 <= shift, frac_bits <= 62; n_tok, n_heads * head_dim < 2^24; n_pos < 2^31. */
+int comet_rotate_share(comet_ctx* ctx, int party, const uint64_t* x_i, int64_t ldx,
+                       const int32_t* positions, const uint64_t* cos_t, const uint64_t* sin_t,
+                       int64_t n_pos, int64_t n_tok, int n_heads, int head_dim, int rot_dim,
+                       int interleaved, int shift, int frac_bits, const uint64_t* m_i, uint64_t* out);
+
+/* A batch of sequences over a paged cache (the struct in HOST memory, read before the call returns; what it
+ * points to on the device).  Sequence s owns the tokens q_start[s] .. q_start[s + 1) of the n_tok new ones and
+ * kv_len[s] cached rows, its new tokens the last of them; its key j lies in slot
+ *     block_table[s * max_pages + j / page_size] * page_size + j % page_size.
+ * ROW (t, h) -- token t, query head h, number t * n_heads + h -- belongs to key head h / (n_heads / n_kv_heads) and
+ * SEES the first v(t, h) keys of its sequence: kv_len[s], or with COMET_CAUSAL
+ * max(kv_len[s] - n_q + j + 1, 0) for the j-th of n_q new tokens; none when head_mask (n_tok x n_heads bytes, may be
+ * NULL) has a zero for it.  An n_tok x n_heads x ld matrix holds a word for every row and key; of its rows
+ * only the first v words are ever read or written.  Tokens outside every sequence (padding) are left as they were.
+ * What does not fit stays in bounds: q_start is read as ascending within 0 .. n_tok, kv_len as at most
+ * min(ld, max_pages * page_size), a page id outside 0 .. n_pages - 1 as 0; tokens of a sequence at or beyond the
+ * max_q-th are not computed. */
+typedef struct comet_kv_batch {
+    int32_t n_seq, n_tok;
+    int32_t n_heads, n_kv_heads;    /* n_heads a multiple of n_kv_heads */
+    int32_t page_size, max_pages;   /* page_size a multiple of 16; pages in a row of block_table */
+    int32_t max_q;                  /* host bound on the new tokens of one sequence */
+    int32_t flags;                  /* 0 or COMET_CAUSAL */
+    const int32_t* q_start;         /* n_seq + 1 */
+    const int32_t* kv_len;          /* n_seq */
+    const int32_t* block_table;     /* n_seq x max_pages */
+    const uint8_t* head_mask;
+} comet_kv_batch;
+enum { COMET_CAUSAL = 1 };
+
+/* Queries times cached keys, for every row r = (t, h) and key j < v(r) with the key's cached head row in F and X_i:
+ *     [Z]_i(r, j) = t([C]_i(r, j) + sum_c E(r, c) [X]_i(j, c) + [A]_i(r, c) F(j, c))  -  [M]_i(r, j),
+ * t(.) the share-local rescaling by frac_bits (0: none).  M_i is the mask under which the scores are sent on (NULL:
+ * none).  E, A_i: n_tok x n_heads x d (opened masked queries, and their mask's share); C_i, M_i, Z_i: n_tok x n_heads x
+ * ld; pools: n_pages * page_size slots of n_kv_heads x ldp words.
+ * d and ldp even, 1 <= d <= ldp, d <= 4096; ld even, < 2^24; n_tok * n_heads < 2^31; n_pages * page_size < 2^31.
+ * Z_i may be C_i or M_i; it must not overlap anything else.
+ * ws: comet_workspace_bytes(COMET_OP_SCORES, n_tok * n_heads, d, ld, 0) bytes (0: none). */
+int comet_attention_scores(comet_ctx* ctx, int party, const comet_kv_batch* batch, int d, int ldp,
+                           int64_t n_pages, int64_t ld, int frac_bits, const uint64_t* E,
+                           const uint64_t* A_i, const uint64_t* f_pool, const uint64_t* x_pool,
+                           const uint64_t* C_i, const uint64_t* M_i, uint64_t* Z_i, void* ws,
+                           size_t ws_bytes);
+
+/* Attention weights without an exponential: w = (s + bias)^2 of the scores s, and their sums over a row, by which the
+ * values are divided in the end.  The scores come masked by a square pair, as d_0 + d_1 = s - r (what the two parties
+ * sent each other; d_1 may be NULL: then d_0 is already opened); r_i and r2_i share r and r^2.  For every j < v(row),
+ * with u = d_0 + d_1 + bias:
+ *     w_i = t(r2_i + 2 u r_i + party * u^2 by frac_bits),      out = w_i - m_i,      sums(row) = sum_j w_i.
+ * m_i (NULL: none) is the mask under which the weights are sent on.  d_0 .. m_i, out: n_tok x n_heads x ld; sums:
+ * n_tok x n_heads words, 0 for a row that sees nothing.  out may be any of the inputs.  Of batch only lengths, heads and
+ * flags are used; page_size and max_pages bound kv_len as above. */
+int comet_attention_weights(comet_ctx* ctx, int party, const comet_kv_batch* batch, int64_t ld,
+                            int frac_bits, uint64_t bias, const uint64_t* d_0, const uint64_t* d_1,
+                            const uint64_t* r_i, const uint64_t* r2_i, const uint64_t* m_i,
+                            uint64_t* out, uint64_t* sums);
+
+/* Weights times cached values, for every row r = (t, h) of a sequence and every column c < d:
+ *     [Z]_i(r, c) = t([C]_i(r, c) + sum_{j < v(r)} E(r, j) [X]_i(j, c) + [A]_i(r, j) F(j, c))  -  [M]_i(r, c).
+ * E, A_i: n_tok x n_heads x ld (opened masked weights, and their mask's share); C_i, M_i, Z_i: n_tok x n_heads x d.  A
+ * row that sees nothing is t([C]_i) - [M]_i.  Everything else as in comet_attention_scores, with
+ * ws: comet_workspace_bytes(COMET_OP_VALUES, n_tok * n_heads, ld, d, 0) bytes. */
+int comet_attention_values(comet_ctx* ctx, int party, const comet_kv_batch* batch, int d, int ldp,
+                           int64_t n_pages, int64_t ld, int frac_bits, const uint64_t* E,
+                           const uint64_t* A_i, const uint64_t* f_pool, const uint64_t* x_pool,
+                           const uint64_t* C_i, const uint64_t* M_i, uint64_t* Z_i, void* ws,
+                           size_t ws_bytes);
 
 /* ---- measurement aids (roofline probes; not part of the protocol) ------- */
 

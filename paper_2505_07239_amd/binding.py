@@ -24,7 +24,8 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libcomet_ring.so")
 
 AXIS_COLS, AXIS_ROWS = 0, 1
-OP_COMPACT, OP_SOMM, OP_SIMM = 0, 1, 2
+OP_COMPACT, OP_SOMM, OP_SIMM, OP_SCORES, OP_VALUES = 0, 1, 2, 3, 4
+CAUSAL = 1
 FULL_A, FULL_B, WEIGHTS_NEURON_MAJOR, WEIGHT_PLANES = 1, 2, 4, 8
 TUNE_GEMM_GRID, TUNE_GEMM_CHUNK, TUNE_GEMM_TILE, TUNE_SKINNY, TUNE_SKINNY_SLICES, TUNE_COMPONENTS = 0, 1, 2, 3, 4, 5
 TUNE_TIMING_STRIDE, TUNE_GROUP = 6, 7
@@ -37,6 +38,8 @@ EXPORTS = [
     "comet_somm_share_unopened", "comet_simm_share_unopened",
     "comet_components", "comet_somm_share_blocks", "comet_simm_share_masked",
     "comet_permute_mask", "comet_scatter_cols", "comet_truncate_share",
+    "comet_cache_write", "comet_cache_read", "comet_rotate_share",
+    "comet_attention_scores", "comet_attention_weights", "comet_attention_values",
     "comet_set_tuning", "comet_timing_begin", "comet_timing_end", "comet_probe_mfma_i8", "comet_probe_valu_mac64", "comet_probe_copy",
 ]
 
@@ -92,6 +95,13 @@ def load_library() -> ctypes.CDLL:
     lib.comet_permute_mask.argtypes = [vp, vp, vp, vp, vp, i64, i64, i32, i32]
     lib.comet_scatter_cols.argtypes = [vp, vp, i64, i32, vp, vp, i32, vp, i64]
     lib.comet_truncate_share.argtypes = [vp, i32, vp, vp, sz, i32]
+    lib.comet_cache_write.argtypes = [vp, i32, vp, vp, vp, vp, i64, i64, vp, vp, i64]
+    lib.comet_cache_read.argtypes = [vp, i32, vp, vp, vp, i64, i64, i64, vp, vp]
+    lib.comet_rotate_share.argtypes = [vp, i32, vp, i64, vp, vp, vp, i64, i64, i32, i32, i32, i32, i32, i32, vp, vp]
+    product = [vp, i32, ctypes.POINTER(_Batch), i32, i32, i64, i64, i32, vp, vp, vp, vp, vp, vp, vp, vp, sz]
+    lib.comet_attention_scores.argtypes = product
+    lib.comet_attention_values.argtypes = product
+    lib.comet_attention_weights.argtypes = [vp, i32, ctypes.POINTER(_Batch), i64, i32, ctypes.c_uint64, vp, vp, vp, vp, vp, vp, vp]
     lib.comet_probe_mfma_i8.argtypes = [vp, i32, i32, i32, vp, ctypes.POINTER(ctypes.c_double)]
     lib.comet_probe_valu_mac64.argtypes = [vp, i32, i32, vp, ctypes.POINTER(ctypes.c_double)]
     lib.comet_probe_copy.argtypes = [vp, vp, vp, sz]
@@ -201,6 +211,50 @@ def _index_list(blk_idx, n_blk_dev, n_blk_cap: int, required: bool):
     if n_blk_dev is not None:
         if n_blk_dev.dtype != torch.int32 or not n_blk_dev.is_cuda or n_blk_dev.numel() < 1:
             raise TypeError("n_blk_dev must be an int32 tensor on the GPU")
+
+
+class _Batch(ctypes.Structure):
+    """``comet_kv_batch``."""
+    _fields_ = [("n_seq", ctypes.c_int32), ("n_tok", ctypes.c_int32), ("n_heads", ctypes.c_int32),
+                ("n_kv_heads", ctypes.c_int32), ("page_size", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+                ("max_q", ctypes.c_int32), ("flags", ctypes.c_int32), ("q_start", ctypes.c_void_p),
+                ("kv_len", ctypes.c_void_p), ("block_table", ctypes.c_void_p), ("head_mask", ctypes.c_void_p)]
+
+
+class KVBatch:
+    """A batch of sequences over a paged cache, for the ``attention_*`` calls (``comet_kv_batch``): which of the
+    ``n_tok`` new tokens belong to which sequence, how many cached rows each has, and where its pages are.
+
+    ``q_start`` [n_seq + 1], ``kv_len`` [n_seq] and ``block_table`` [n_seq, max_pages] are int32 tensors on the
+    GPU, ``head_mask`` [n_tok, n_heads] uint8 (None: every head is active).  They are read when a call runs, so a
+    program that generates tokens keeps one batch and updates the tensors in place.  ``max_q`` bounds the
+    new tokens of one sequence."""
+
+    def __init__(self, n_tok, n_heads, n_kv_heads, q_start, kv_len, block_table, page_size, max_q, causal=True,
+                 head_mask=None):
+        for t, what in ((q_start, "q_start"), (kv_len, "kv_len"), (block_table, "block_table")):
+            _ints(t, what)
+        n_seq = kv_len.numel()
+        if kv_len.dim() != 1 or q_start.shape != (n_seq + 1,) or block_table.dim() != 2 or block_table.shape[0] != n_seq:
+            raise ValueError("expected q_start [n_seq + 1], kv_len [n_seq] and block_table [n_seq, max_pages]")
+        if head_mask is not None:
+            if head_mask.dtype != torch.uint8 or not head_mask.is_cuda or not head_mask.is_contiguous():
+                raise TypeError("head_mask must be a contiguous uint8 tensor on the GPU")
+            _shape(head_mask, (n_tok, n_heads), "head_mask")
+        tensors = [t for t in (q_start, kv_len, block_table, head_mask) if t is not None]
+        if len({t.device for t in tensors}) != 1:
+            raise ValueError("the tensors of a batch must be on one device")
+        self.tensors, self.device = tensors, kv_len.device.index
+        self.n_tok, self.n_heads, self.n_kv_heads, self.page_size = n_tok, n_heads, n_kv_heads, page_size
+        self.struct = _Batch(n_seq, n_tok, n_heads, n_kv_heads, page_size, block_table.shape[1], max_q,
+                             CAUSAL if causal else 0, *[_ptr(t) for t in (q_start, kv_len, block_table, head_mask)])
+        self.ref = ctypes.byref(self.struct)
+
+
+def _ints(t: torch.Tensor, what: str) -> torch.Tensor:
+    if t.dtype != torch.int32 or not t.is_cuda or not t.is_contiguous():
+        raise TypeError("%s must be a contiguous int32 tensor on the GPU" % what)
+    return t
 
 
 def _shape(t: torch.Tensor, shape, what: str):
@@ -623,6 +677,140 @@ class Context:
         self._sync_stream()
         self._check(self.lib.comet_truncate_share(self.h, party, _ptr(z), _ptr(out), z.numel(), frac_bits))
         return out
+
+    # ---- (6) attention over a cache of shares ----
+    def _here(self, *tensors):
+        """Every tensor (None: absent) is on the context's device."""
+        for t in tensors:
+            if t is not None and t.device.index != self.device:
+                raise ValueError("operands must be on the context's device, cuda:%d" % self.device)
+
+    def cache_write(self, party, d_0, d_1, b_i, slots, f_pool, x_pool):
+        """F[slots] = d_0 + d_1 and X_i[slots] = b_i + party * F, in place.  ``d_0``, ``d_1``, ``b_i``: [n_tok, ...]
+        with the words of a slot; ``slots`` int32 [n_tok], -1 for padding; pools of any shape whose elements are n_slots
+        times the words of a slot."""
+        _words(d_0, "d_0"), _words(d_1, "d_1"), _words(b_i, "b_i"), _words(f_pool, "f_pool"), _words(x_pool, "x_pool")
+        n_tok, width, n_slots = self._rows(slots, d_0, f_pool, x_pool)
+        if d_1.shape != d_0.shape or b_i.shape != d_0.shape:
+            raise ValueError("d_0, d_1 and b_i must have one shape")
+        self._here(d_0, d_1, b_i, slots, f_pool, x_pool)
+        self._sync_stream()
+        self._check(self.lib.comet_cache_write(self.h, party, _ptr(d_0), _ptr(d_1), _ptr(b_i), _ptr(slots), n_tok, width,
+                                               _ptr(f_pool), _ptr(x_pool), n_slots))
+
+    def cache_read(self, party, f_pool, x_pool, slots, width=None, out=None):
+        """(F[slots], X_i[slots] - party * F[slots]): cached rows as E and A_i of a share product, [n_tok, width].
+        ``width``: words of a slot (default: those of ``out``, or the pools' elements per entry of their first axis)."""
+        _words(f_pool, "f_pool"), _words(x_pool, "x_pool"), _ints(slots, "slots")
+        if out is None:
+            width = f_pool[0].numel() if width is None else width
+            shape = (slots.numel(), width)
+            out = tuple(torch.zeros(shape, dtype=torch.int64, device=f_pool.device) for _ in (0, 1))
+        e, a_i = out
+        _words(e, "e"), _words(a_i, "a_i")
+        n_tok, n_words, n_slots = self._rows(slots, e, f_pool, x_pool)
+        if a_i.shape != e.shape or (width is not None and n_words != width):
+            raise ValueError("e and a_i must have one shape, a slot's words per token")
+        self._here(f_pool, x_pool, slots, e, a_i)
+        self._sync_stream()
+        self._check(self.lib.comet_cache_read(self.h, party, _ptr(f_pool), _ptr(x_pool), _ptr(slots), n_tok, n_words, n_slots,
+                                              _ptr(e), _ptr(a_i)))
+        return e, a_i
+
+    @staticmethod
+    def _rows(slots, rows, f_pool, x_pool):
+        """(tokens, words of a slot, slots) of a cache call."""
+        _ints(slots, "slots")
+        n_tok = slots.numel()
+        if slots.dim() != 1 or rows.dim() < 2 or rows.shape[0] != n_tok:
+            raise ValueError("expected one slot and one row per token")
+        width = rows.shape[1:].numel()
+        if f_pool.numel() != x_pool.numel() or (width and f_pool.numel() % width != 0):
+            raise ValueError("the pools must hold the same number of words, a whole number of slots")
+        return n_tok, width, f_pool.numel() // width if width else 0
+
+    def rotate_share(self, party, x_i, positions, cos, sin, n_heads, shift=0, frac_bits=16, m_i=None, interleaved=False,
+                     out=None):
+        """Rescaling, position rotation and masking of queries or keys: ``x_i`` [n_tok, n_heads * head_dim], possibly a column
+        range of a wider matrix; ``cos``, ``sin`` [n_pos, rot_dim / 2] fixed-point words; ``positions`` int32 [n_tok]."""
+        if x_i.dtype != torch.int64 or not x_i.is_cuda or x_i.dim() != 2 or (x_i.shape[1] > 1 and x_i.stride(1) != 1):
+            raise TypeError("x_i must be a 2-D int64 tensor on the GPU with contiguous rows")
+        _words(cos, "cos"), _words(sin, "sin"), _ints(positions, "positions")
+        n_tok, width = x_i.shape
+        if n_heads < 1 or width % n_heads != 0:
+            raise ValueError("x_i must have n_heads * head_dim columns")
+        if cos.dim() != 2 or sin.shape != cos.shape or positions.shape != (n_tok,):
+            raise ValueError("expected cos and sin [n_pos, rot_dim / 2] and one position per token")
+        if m_i is not None:
+            _shape(_words(m_i, "m_i"), (n_tok, width), "m_i")
+        out = torch.empty((n_tok, width), dtype=torch.int64, device=x_i.device) if out is None else _words(out, "out")
+        _shape(out, (n_tok, width), "out")
+        ldx = x_i.stride(0) if n_tok > 1 else width
+        self._here(x_i, positions, cos, sin, m_i, out)
+        self._sync_stream()
+        self._check(self.lib.comet_rotate_share(self.h, party, _ptr(x_i), ldx, _ptr(positions), _ptr(cos), _ptr(sin),
+                                                cos.shape[0], n_tok, n_heads, width // n_heads, 2 * cos.shape[1],
+                                                1 if interleaved else 0, shift, frac_bits, _ptr(m_i), _ptr(out)))
+        return out
+
+    def _product(self, call, op, party, batch, e, a_i, f_pool, x_pool, c_i, frac_bits, m_i, out):
+        for t, what in ((e, "E"), (a_i, "A_i"), (f_pool, "f_pool"), (x_pool, "x_pool"), (c_i, "C_i")):
+            _words(t, what)
+        if e.dim() != 3 or c_i.dim() != 3 or f_pool.dim() != 4:
+            raise ValueError("expected E and C_i [n_tok, n_heads, .] and pools [n_pages, page_size, n_kv_heads, .]")
+        left, right = (batch.n_tok, batch.n_heads, e.shape[2]), (batch.n_tok, batch.n_heads, c_i.shape[2])
+        n_pages, ldp = f_pool.shape[0], f_pool.shape[3]
+        _shape(e, left, "E"), _shape(a_i, left, "A_i"), _shape(c_i, right, "C_i")
+        _shape(f_pool, (n_pages, batch.page_size, batch.n_kv_heads, ldp), "f_pool")
+        _shape(x_pool, f_pool.shape, "x_pool")
+        if m_i is not None:
+            _shape(_words(m_i, "M_i"), right, "M_i")
+        out = torch.zeros(right, dtype=torch.int64, device=e.device) if out is None else _words(out, "out")
+        _shape(out, right, "out")
+        self._here(e, a_i, f_pool, x_pool, c_i, m_i, out, batch.tensors[0])
+        d, ld = (left[2], right[2]) if op == OP_SCORES else (right[2], left[2])
+        need = workspace_bytes(op, batch.n_tok * batch.n_heads, left[2], right[2], 0)
+        # (an allocation of the call's own: a graph that captures it keeps it, and no two calls share it)
+        ws = torch.empty(need, dtype=torch.uint8, device=e.device) if need else None
+        self._sync_stream()
+        self._check(call(self.h, party, batch.ref, d, ldp, n_pages, ld, frac_bits, _ptr(e), _ptr(a_i), _ptr(f_pool),
+                         _ptr(x_pool), _ptr(c_i), _ptr(m_i), _ptr(out), _ptr(ws), need))
+        return out
+
+    def attention_scores(self, party, batch, e, a_i, f_pool, x_pool, c_i, frac_bits=0, m_i=None, out=None):
+        """Share of queries times cached keys, rescaled and masked: ``e``, ``a_i`` [n_tok, n_heads, d]; pools
+        [n_pages, page_size, n_kv_heads, >= d]; ``c_i``, ``m_i`` and the result [n_tok, n_heads, ld].  Keys that a row
+        does not see are left as they were in ``out`` (zero in a result that the call allocates)."""
+        return self._product(self.lib.comet_attention_scores, OP_SCORES, party, batch, e, a_i, f_pool, x_pool, c_i, frac_bits,
+                             m_i, out)
+
+    def attention_values(self, party, batch, e, a_i, f_pool, x_pool, c_i, frac_bits=0, m_i=None, out=None):
+        """Share of weights times cached values, rescaled and masked: ``e``, ``a_i`` [n_tok, n_heads, ld]; ``c_i``,
+        ``m_i`` and the result [n_tok, n_heads, d]; the first d words of a head's row in the pools are its values."""
+        return self._product(self.lib.comet_attention_values, OP_VALUES, party, batch, e, a_i, f_pool, x_pool, c_i, frac_bits,
+                             m_i, out)
+
+    def attention_weights(self, party, batch, d_0, d_1, r_i, r2_i, bias, frac_bits=16, m_i=None, out=None):
+        """(shares of w = (s + bias)^2 - m, shares of the row sums of w) from masked scores d_0 + d_1 = s - r (``d_1``
+        None: ``d_0`` is already opened) and a square pair (r, r^2); all [n_tok, n_heads, ld].  ``out``: (weights, sums)."""
+        for t, what in ((d_0, "d_0"), (r_i, "r_i"), (r2_i, "r2_i")):
+            _words(t, what)
+        if d_0.dim() != 3:
+            raise ValueError("expected operands [n_tok, n_heads, ld]")
+        shape = (batch.n_tok, batch.n_heads, d_0.shape[2])
+        for t, what in ((d_0, "d_0"), (d_1, "d_1"), (r_i, "r_i"), (r2_i, "r2_i"), (m_i, "m_i")):
+            if t is not None:
+                _shape(_words(t, what), shape, what)
+        if out is None:
+            out = tuple(torch.zeros(s, dtype=torch.int64, device=d_0.device) for s in (shape, shape[:2]))
+        w, sums = out
+        _shape(_words(w, "out"), shape, "out"), _shape(_words(sums, "sums"), shape[:2], "sums")
+        self._here(d_0, d_1, r_i, r2_i, m_i, w, sums, batch.tensors[0])
+        self._sync_stream()
+        self._check(self.lib.comet_attention_weights(self.h, party, batch.ref, shape[2], frac_bits, bias & (2 ** 64 - 1),
+                                                     _ptr(d_0), _ptr(d_1), _ptr(r_i), _ptr(r2_i), _ptr(m_i), _ptr(w),
+                                                     _ptr(sums)))
+        return w, sums
 
     # ---- probes ----
     def set_tuning(self, key: int, value: int):

@@ -1,0 +1,236 @@
+// Attention over a cache of shares: one party's share of the products of queries and keys and of weights and values
+// (Eq. 1 with the cache's own share in the place of B_i), and the squared weights between them.
+#include "kv_batch.h"
+
+using namespace comet_attn;
+
+namespace {
+
+constexpr int GT = 256;
+
+struct ProductParams {
+    Batch b;
+    int party, d, ldp, frac;
+    const u64* E;
+    const u64* A;
+    const u64* F;
+    const u64* X;
+    const u64* C;
+    const u64* M;
+    u64* Z;
+};
+
+// One thread per (row, key).
+__global__ __launch_bounds__(GT) void scores_kernel(ProductParams p, int chunks) {
+    const Batch& b = p.b;
+    unsigned w = blockIdx.x;
+    const int chunk = (int)(w % (unsigned)chunks); w /= (unsigned)chunks;
+    const int h = (int)(w % (unsigned)b.n_heads); w /= (unsigned)b.n_heads;
+    const int j = (int)(w % (unsigned)b.max_q);
+    const Sequence sq(b, (int)(w / (unsigned)b.max_q));
+    if (j >= sq.nq) return;
+    const int key = chunk * GT + threadIdx.x;
+    if (key >= sq.sees(b, j, h)) return;
+    const size_t row = (size_t)(sq.q0 + j) * b.n_heads + h;
+    const size_t at = (sq.slot(b, key) * b.n_kv_heads + h / b.group) * p.ldp;
+    u64 z = p.C[row * b.ld + key];
+    for (int c = 0; c < p.d; ++c) z += p.E[row * p.d + c] * p.X[at + c] + p.A[row * p.d + c] * p.F[at + c];
+    z = rescale(p.party, z, p.frac);
+    if (p.M) z -= p.M[row * b.ld + key];
+    p.Z[row * b.ld + key] = z;
+}
+
+// One thread per (row, column).
+__global__ __launch_bounds__(GT) void values_kernel(ProductParams p, int chunks) {
+    const Batch& b = p.b;
+    unsigned w = blockIdx.x;
+    const int chunk = (int)(w % (unsigned)chunks); w /= (unsigned)chunks;
+    const int h = (int)(w % (unsigned)b.n_heads); w /= (unsigned)b.n_heads;
+    const int j = (int)(w % (unsigned)b.max_q);
+    const Sequence sq(b, (int)(w / (unsigned)b.max_q));
+    if (j >= sq.nq) return;
+    const int c = chunk * GT + threadIdx.x;
+    if (c >= p.d) return;
+    const int v = sq.sees(b, j, h);
+    const size_t row = (size_t)(sq.q0 + j) * b.n_heads + h;
+    u64 z = p.C[row * p.d + c];
+    for (int key = 0; key < v; ++key) {
+        const size_t at = (sq.slot(b, key) * b.n_kv_heads + h / b.group) * p.ldp + c;
+        z += p.E[row * b.ld + key] * p.X[at] + p.A[row * b.ld + key] * p.F[at];
+    }
+    z = rescale(p.party, z, p.frac);
+    if (p.M) z -= p.M[row * p.d + c];
+    p.Z[row * p.d + c] = z;
+}
+
+struct WeightParams {
+    Batch b;
+    int party, frac;
+    u64 bias;
+    const u64* d0;
+    const u64* d1;
+    const u64* r;
+    const u64* r2;
+    const u64* m;
+    u64* out;
+    u64* sums;
+};
+
+// One workgroup per row.
+__global__ __launch_bounds__(GT) void weights_kernel(WeightParams p) {
+    const Batch& b = p.b;
+    unsigned w = blockIdx.x;
+    const int h = (int)(w % (unsigned)b.n_heads); w /= (unsigned)b.n_heads;
+    const int j = (int)(w % (unsigned)b.max_q);
+    const Sequence sq(b, (int)(w / (unsigned)b.max_q));
+    if (j >= sq.nq) return;
+    const int v = sq.sees(b, j, h);
+    const size_t row = (size_t)(sq.q0 + j) * b.n_heads + h;
+    u64 sum = 0;
+    for (int key = threadIdx.x; key < v; key += GT) {
+        const size_t at = row * b.ld + key;
+        const u64 u = p.d0[at] + (p.d1 ? p.d1[at] : 0) + p.bias;
+        u64 x = p.r2[at] + 2 * u * p.r[at];
+        if (p.party) x += u * u;
+        x = rescale(p.party, x, p.frac);
+        sum += x;
+        p.out[at] = p.m ? x - p.m[at] : x;
+    }
+    __shared__ u64 part[GT];
+    part[threadIdx.x] = sum;
+    __syncthreads();
+    for (int n = GT / 2; n > 0; n /= 2) {
+        if ((int)threadIdx.x < n) part[threadIdx.x] += part[threadIdx.x + n];
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) p.sums[row] = part[0];
+}
+
+// Checks of a batch; fills the device view.  COMET_OK with n_tok == 0 or n_seq == 0 means: nothing to do.
+int make_batch(comet_ctx* ctx, const char* what, const comet_kv_batch* in, int64_t n_pages, int64_t ld, Batch* b) {
+    if (!in) return comet_fail(ctx, COMET_EINVAL, "%s: null batch", what);
+    if (in->n_seq < 0 || in->n_tok < 0 || in->n_heads < 1 || in->n_kv_heads < 1 || in->n_heads % in->n_kv_heads != 0 ||
+        in->max_q < 0 || in->max_pages < 0 || in->page_size < 16 || in->page_size % 16 != 0 || (in->flags & ~COMET_CAUSAL) != 0)
+        return comet_fail(ctx, COMET_EINVAL, "%s: bad batch (n_heads must be a multiple of n_kv_heads, page_size of 16)", what);
+    if (ld < 0 || (ld & 1) || n_pages < 0) return comet_fail(ctx, COMET_EINVAL, "%s: ld must be even and not negative", what);
+    if (ld > COMET_DIM_MAX || n_pages > 0x7fffffffll || n_pages * in->page_size > 0x7fffffffll ||
+        (int64_t)in->n_tok * in->n_heads > 0x7fffffffll || (int64_t)in->n_seq * in->max_q > COMET_DIM_MAX)
+        return comet_fail(ctx, COMET_ECAP, "%s: ld and n_seq * max_q must stay below 2^24, rows and slots below 2^31", what);
+    if (in->n_seq > 0 && in->n_tok > 0 && (!in->q_start || !in->kv_len || (in->max_pages > 0 && !in->block_table)))
+        return comet_fail(ctx, COMET_EINVAL, "%s: null pointer in the batch", what);
+    b->n_seq = in->n_seq; b->n_tok = in->n_tok; b->n_heads = in->n_heads; b->n_kv_heads = in->n_kv_heads;
+    b->group = in->n_heads / in->n_kv_heads;
+    b->page_size = in->page_size; b->max_pages = in->max_pages; b->n_pages = (int)n_pages;
+    b->max_q = in->max_q; b->causal = (in->flags & COMET_CAUSAL) != 0;
+    b->ld = (int)ld;
+    const int64_t cap = (int64_t)in->max_pages * in->page_size;
+    b->kv_cap = (int)(cap < ld ? cap : ld);
+    b->q_start = in->q_start; b->kv_len = in->kv_len; b->block_table = in->block_table; b->head_mask = in->head_mask;
+    return COMET_OK;
+}
+
+int make_product(comet_ctx* ctx, const char* what, int party, const comet_kv_batch* batch, int d, int ldp, int64_t n_pages,
+                 int64_t ld, int frac_bits, const uint64_t* E, const uint64_t* A_i, const uint64_t* f_pool,
+                 const uint64_t* x_pool, const uint64_t* C_i, const uint64_t* M_i, uint64_t* Z_i, ProductParams* p) {
+    if ((party != 0 && party != 1) || frac_bits < 0 || frac_bits > 62)
+        return comet_fail(ctx, COMET_EINVAL, "%s: party must be 0 or 1, 0 <= frac_bits <= 62", what);
+    const int rc = make_batch(ctx, what, batch, n_pages, ld, &p->b);
+    if (rc != COMET_OK) return rc;
+    if (d < 1 || (d & 1) || (ldp & 1) || ldp < d) return comet_fail(ctx, COMET_EINVAL, "%s: d and ldp must be even, 1 <= d <= ldp", what);
+    if (d > 4096 || ldp > COMET_DIM_MAX) return comet_fail(ctx, COMET_ECAP, "%s: d must be at most 4096", what);
+    if (p->b.n_tok == 0 || p->b.n_seq == 0 || p->b.max_q == 0) return COMET_OK;
+    if (n_pages < 1 && p->b.kv_cap > 0) return comet_fail(ctx, COMET_EINVAL, "%s: empty pools", what);
+    const void* ptrs[] = {E, A_i, f_pool, x_pool, C_i, Z_i};
+    for (const void* q : ptrs) {
+        if (!q) return comet_fail(ctx, COMET_EINVAL, "%s: null pointer", what);
+        if (!comet_aligned16(q)) return comet_fail(ctx, COMET_EALIGN, "%s: operands must be 16-byte aligned", what);
+    }
+    if (M_i && !comet_aligned16(M_i)) return comet_fail(ctx, COMET_EALIGN, "%s: operands must be 16-byte aligned", what);
+    p->party = party; p->d = d; p->ldp = ldp; p->frac = frac_bits;
+    p->E = (const u64*)E; p->A = (const u64*)A_i; p->F = (const u64*)f_pool; p->X = (const u64*)x_pool;
+    p->C = (const u64*)C_i; p->M = (const u64*)M_i; p->Z = (u64*)Z_i;
+    return COMET_OK;
+}
+
+}  // namespace
+
+size_t comet_attention_workspace_bytes(int op, int64_t m, int64_t k, int64_t n) {
+    (void)op; (void)m; (void)k; (void)n;
+    return 0;
+}
+
+extern "C" {
+
+int comet_attention_scores(comet_ctx* ctx, int party, const comet_kv_batch* batch, int d, int ldp, int64_t n_pages, int64_t ld,
+                           int frac_bits, const uint64_t* E, const uint64_t* A_i, const uint64_t* f_pool, const uint64_t* x_pool,
+                           const uint64_t* C_i, const uint64_t* M_i, uint64_t* Z_i, void* ws, size_t ws_bytes) {
+    const char* what = "comet_attention_scores";
+    COMET_CHECK_CTX(ctx);
+    (void)ws; (void)ws_bytes;
+    ProductParams p;
+    const int rc = make_product(ctx, what, party, batch, d, ldp, n_pages, ld, frac_bits, E, A_i, f_pool, x_pool, C_i, M_i, Z_i, &p);
+    if (rc != COMET_OK) return rc;
+    const Batch& b = p.b;
+    if (b.n_tok == 0 || b.n_seq == 0 || b.max_q == 0 || b.kv_cap == 0) return COMET_OK;
+    comet_device_guard guard(ctx);
+    if (!guard.ok) return comet_fail(ctx, COMET_EDEVICE, "%s: cannot select device", what);
+    const int chunks = (b.kv_cap + GT - 1) / GT;
+    const int64_t grid = (int64_t)b.n_seq * b.max_q * b.n_heads * chunks;
+    if (grid > 0x7fffffffll) return comet_fail(ctx, COMET_ECAP, "%s: too many rows", what);
+    hipLaunchKernelGGL(scores_kernel, dim3((unsigned)grid), dim3(GT), 0, ctx->stream, p, chunks);
+    COMET_LAUNCH_CHECK(ctx, what);
+    return COMET_OK;
+}
+
+int comet_attention_values(comet_ctx* ctx, int party, const comet_kv_batch* batch, int d, int ldp, int64_t n_pages, int64_t ld,
+                           int frac_bits, const uint64_t* E, const uint64_t* A_i, const uint64_t* f_pool, const uint64_t* x_pool,
+                           const uint64_t* C_i, const uint64_t* M_i, uint64_t* Z_i, void* ws, size_t ws_bytes) {
+    const char* what = "comet_attention_values";
+    COMET_CHECK_CTX(ctx);
+    (void)ws; (void)ws_bytes;
+    ProductParams p;
+    const int rc = make_product(ctx, what, party, batch, d, ldp, n_pages, ld, frac_bits, E, A_i, f_pool, x_pool, C_i, M_i, Z_i, &p);
+    if (rc != COMET_OK) return rc;
+    const Batch& b = p.b;
+    if (b.n_tok == 0 || b.n_seq == 0 || b.max_q == 0) return COMET_OK;
+    comet_device_guard guard(ctx);
+    if (!guard.ok) return comet_fail(ctx, COMET_EDEVICE, "%s: cannot select device", what);
+    const int chunks = (d + GT - 1) / GT;
+    const int64_t grid = (int64_t)b.n_seq * b.max_q * b.n_heads * chunks;
+    if (grid > 0x7fffffffll) return comet_fail(ctx, COMET_ECAP, "%s: too many rows", what);
+    hipLaunchKernelGGL(values_kernel, dim3((unsigned)grid), dim3(GT), 0, ctx->stream, p, chunks);
+    COMET_LAUNCH_CHECK(ctx, what);
+    return COMET_OK;
+}
+
+int comet_attention_weights(comet_ctx* ctx, int party, const comet_kv_batch* batch, int64_t ld, int frac_bits, uint64_t bias,
+                            const uint64_t* d_0, const uint64_t* d_1, const uint64_t* r_i, const uint64_t* r2_i,
+                            const uint64_t* m_i, uint64_t* out, uint64_t* sums) {
+    const char* what = "comet_attention_weights";
+    COMET_CHECK_CTX(ctx);
+    if ((party != 0 && party != 1) || frac_bits < 0 || frac_bits > 62)
+        return comet_fail(ctx, COMET_EINVAL, "%s: party must be 0 or 1, 0 <= frac_bits <= 62", what);
+    WeightParams p;
+    const int rc = make_batch(ctx, what, batch, 1, ld, &p.b);
+    if (rc != COMET_OK) return rc;
+    const Batch& b = p.b;
+    if (b.n_tok == 0 || b.n_seq == 0 || b.max_q == 0) return COMET_OK;
+    const void* ptrs[] = {d_0, r_i, r2_i, out, sums};
+    for (const void* q : ptrs)
+        if (!q) return comet_fail(ctx, COMET_EINVAL, "%s: null pointer", what);
+    const void* all[] = {d_0, d_1, r_i, r2_i, m_i, out, sums};
+    for (const void* q : all)
+        if (q && !comet_aligned16(q)) return comet_fail(ctx, COMET_EALIGN, "%s: operands must be 16-byte aligned", what);
+    comet_device_guard guard(ctx);
+    if (!guard.ok) return comet_fail(ctx, COMET_EDEVICE, "%s: cannot select device", what);
+    p.party = party; p.frac = frac_bits; p.bias = bias;
+    p.d0 = (const u64*)d_0; p.d1 = (const u64*)d_1; p.r = (const u64*)r_i; p.r2 = (const u64*)r2_i; p.m = (const u64*)m_i;
+    p.out = (u64*)out; p.sums = (u64*)sums;
+    const int64_t grid = (int64_t)b.n_seq * b.max_q * b.n_heads;
+    if (grid > 0x7fffffffll) return comet_fail(ctx, COMET_ECAP, "%s: too many rows", what);
+    hipLaunchKernelGGL(weights_kernel, dim3((unsigned)grid), dim3(GT), 0, ctx->stream, p);
+    COMET_LAUNCH_CHECK(ctx, what);
+    return COMET_OK;
+}
+
+}  // extern "C"

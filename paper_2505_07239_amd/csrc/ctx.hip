@@ -3,6 +3,7 @@
 
 size_t comet_compact_workspace_bytes(int64_t n_tok, int64_t nb);
 size_t comet_gemm_workspace_bytes(int64_t m, int64_t kc_cap, int64_t n_cap);
+size_t comet_attention_workspace_bytes(int op, int64_t m, int64_t k, int64_t n);
 
 extern "C" {
 
@@ -143,6 +144,8 @@ size_t comet_workspace_bytes(int op, int64_t m, int64_t k, int64_t n, int bs) {
         case COMET_OP_COMPACT: return comet_compact_workspace_bytes(m, n);
         case COMET_OP_SOMM:
         case COMET_OP_SIMM: return comet_gemm_workspace_bytes(m, k, n);
+        case COMET_OP_SCORES:
+        case COMET_OP_VALUES: return comet_attention_workspace_bytes(op, m, k, n);
         default: return 0;
     }
 }
