@@ -1,67 +1,12 @@
-// Attention over a cache of shares: one party's share of the products of queries and keys and of weights and values
-// (Eq. 1 with the cache's own share in the place of B_i), and the squared weights between them.
-#include "kv_batch.h"
+// Attention over a cache of shares: the entry points of the products (attention_scores.hip, attention_values.hip), and the
+// squared weights between them.
+#include "attention_tile.h"
 
 using namespace comet_attn;
 
 namespace {
 
 constexpr int GT = 256;
-
-struct ProductParams {
-    Batch b;
-    int party, d, ldp, frac;
-    const u64* E;
-    const u64* A;
-    const u64* F;
-    const u64* X;
-    const u64* C;
-    const u64* M;
-    u64* Z;
-};
-
-// One thread per (row, key).
-__global__ __launch_bounds__(GT) void scores_kernel(ProductParams p, int chunks) {
-    const Batch& b = p.b;
-    unsigned w = blockIdx.x;
-    const int chunk = (int)(w % (unsigned)chunks); w /= (unsigned)chunks;
-    const int h = (int)(w % (unsigned)b.n_heads); w /= (unsigned)b.n_heads;
-    const int j = (int)(w % (unsigned)b.max_q);
-    const Sequence sq(b, (int)(w / (unsigned)b.max_q));
-    if (j >= sq.nq) return;
-    const int key = chunk * GT + threadIdx.x;
-    if (key >= sq.sees(b, j, h)) return;
-    const size_t row = (size_t)(sq.q0 + j) * b.n_heads + h;
-    const size_t at = (sq.slot(b, key) * b.n_kv_heads + h / b.group) * p.ldp;
-    u64 z = p.C[row * b.ld + key];
-    for (int c = 0; c < p.d; ++c) z += p.E[row * p.d + c] * p.X[at + c] + p.A[row * p.d + c] * p.F[at + c];
-    z = rescale(p.party, z, p.frac);
-    if (p.M) z -= p.M[row * b.ld + key];
-    p.Z[row * b.ld + key] = z;
-}
-
-// One thread per (row, column).
-__global__ __launch_bounds__(GT) void values_kernel(ProductParams p, int chunks) {
-    const Batch& b = p.b;
-    unsigned w = blockIdx.x;
-    const int chunk = (int)(w % (unsigned)chunks); w /= (unsigned)chunks;
-    const int h = (int)(w % (unsigned)b.n_heads); w /= (unsigned)b.n_heads;
-    const int j = (int)(w % (unsigned)b.max_q);
-    const Sequence sq(b, (int)(w / (unsigned)b.max_q));
-    if (j >= sq.nq) return;
-    const int c = chunk * GT + threadIdx.x;
-    if (c >= p.d) return;
-    const int v = sq.sees(b, j, h);
-    const size_t row = (size_t)(sq.q0 + j) * b.n_heads + h;
-    u64 z = p.C[row * p.d + c];
-    for (int key = 0; key < v; ++key) {
-        const size_t at = (sq.slot(b, key) * b.n_kv_heads + h / b.group) * p.ldp + c;
-        z += p.E[row * b.ld + key] * p.X[at] + p.A[row * b.ld + key] * p.F[at];
-    }
-    z = rescale(p.party, z, p.frac);
-    if (p.M) z -= p.M[row * p.d + c];
-    p.Z[row * p.d + c] = z;
-}
 
 struct WeightParams {
     Batch b;
@@ -114,14 +59,15 @@ int make_batch(comet_ctx* ctx, const char* what, const comet_kv_batch* in, int64
         return comet_fail(ctx, COMET_EINVAL, "%s: bad batch (n_heads must be a multiple of n_kv_heads, page_size of 16)", what);
     if (ld < 0 || (ld & 1) || n_pages < 0) return comet_fail(ctx, COMET_EINVAL, "%s: ld must be even and not negative", what);
     if (ld > COMET_DIM_MAX || n_pages > 0x7fffffffll || n_pages * in->page_size > 0x7fffffffll ||
-        (int64_t)in->n_tok * in->n_heads > 0x7fffffffll || (int64_t)in->n_seq * in->max_q > COMET_DIM_MAX)
-        return comet_fail(ctx, COMET_ECAP, "%s: ld and n_seq * max_q must stay below 2^24, rows and slots below 2^31", what);
+        (int64_t)in->n_tok * in->n_heads > 0x7fffffffll || (int64_t)in->n_seq * in->max_q > COMET_DIM_MAX ||
+        (int64_t)in->n_seq * in->n_kv_heads > COMET_DIM_MAX)
+        return comet_fail(ctx, COMET_ECAP, "%s: ld, n_seq * max_q and n_seq * n_kv_heads must stay below 2^24, rows and slots below 2^31", what);
     if (in->n_seq > 0 && in->n_tok > 0 && (!in->q_start || !in->kv_len || (in->max_pages > 0 && !in->block_table)))
         return comet_fail(ctx, COMET_EINVAL, "%s: null pointer in the batch", what);
     b->n_seq = in->n_seq; b->n_tok = in->n_tok; b->n_heads = in->n_heads; b->n_kv_heads = in->n_kv_heads;
     b->group = in->n_heads / in->n_kv_heads;
     b->page_size = in->page_size; b->max_pages = in->max_pages; b->n_pages = (int)n_pages;
-    b->max_q = in->max_q; b->causal = (in->flags & COMET_CAUSAL) != 0;
+    b->max_q = in->max_q < in->n_tok ? in->max_q : in->n_tok; b->causal = (in->flags & COMET_CAUSAL) != 0;
     b->ld = (int)ld;
     const int64_t cap = (int64_t)in->max_pages * in->page_size;
     b->kv_cap = (int)(cap < ld ? cap : ld);
@@ -137,7 +83,8 @@ int make_product(comet_ctx* ctx, const char* what, int party, const comet_kv_bat
     const int rc = make_batch(ctx, what, batch, n_pages, ld, &p->b);
     if (rc != COMET_OK) return rc;
     if (d < 1 || (d & 1) || (ldp & 1) || ldp < d) return comet_fail(ctx, COMET_EINVAL, "%s: d and ldp must be even, 1 <= d <= ldp", what);
-    if (d > 4096 || ldp > COMET_DIM_MAX) return comet_fail(ctx, COMET_ECAP, "%s: d must be at most 4096", what);
+    if (d > MAX_D || (int64_t)p->b.n_kv_heads * ldp > COMET_DIM_MAX)
+        return comet_fail(ctx, COMET_ECAP, "%s: d must be at most %d, a slot's words below 2^24", what, MAX_D);
     if (p->b.n_tok == 0 || p->b.n_seq == 0 || p->b.max_q == 0) return COMET_OK;
     if (n_pages < 1 && p->b.kv_cap > 0) return comet_fail(ctx, COMET_EINVAL, "%s: empty pools", what);
     const void* ptrs[] = {E, A_i, f_pool, x_pool, C_i, Z_i};
@@ -149,14 +96,15 @@ int make_product(comet_ctx* ctx, const char* what, int party, const comet_kv_bat
     p->party = party; p->d = d; p->ldp = ldp; p->frac = frac_bits;
     p->E = (const u64*)E; p->A = (const u64*)A_i; p->F = (const u64*)f_pool; p->X = (const u64*)x_pool;
     p->C = (const u64*)C_i; p->M = (const u64*)M_i; p->Z = (u64*)Z_i;
+    p->part = nullptr;
+    p->tiles = p->groups = p->chunks = p->chunk = 1;
     return COMET_OK;
 }
 
 }  // namespace
 
 size_t comet_attention_workspace_bytes(int op, int64_t m, int64_t k, int64_t n) {
-    (void)op; (void)m; (void)k; (void)n;
-    return 0;
+    return op == COMET_OP_VALUES ? values_workspace_bytes(m, k, n) : 0;
 }
 
 extern "C" {
@@ -166,7 +114,7 @@ int comet_attention_scores(comet_ctx* ctx, int party, const comet_kv_batch* batc
                            const uint64_t* C_i, const uint64_t* M_i, uint64_t* Z_i, void* ws, size_t ws_bytes) {
     const char* what = "comet_attention_scores";
     COMET_CHECK_CTX(ctx);
-    (void)ws; (void)ws_bytes;
+    (void)ws; (void)ws_bytes;                                 // (none is needed)
     ProductParams p;
     const int rc = make_product(ctx, what, party, batch, d, ldp, n_pages, ld, frac_bits, E, A_i, f_pool, x_pool, C_i, M_i, Z_i, &p);
     if (rc != COMET_OK) return rc;
@@ -174,12 +122,7 @@ int comet_attention_scores(comet_ctx* ctx, int party, const comet_kv_batch* batc
     if (b.n_tok == 0 || b.n_seq == 0 || b.max_q == 0 || b.kv_cap == 0) return COMET_OK;
     comet_device_guard guard(ctx);
     if (!guard.ok) return comet_fail(ctx, COMET_EDEVICE, "%s: cannot select device", what);
-    const int chunks = (b.kv_cap + GT - 1) / GT;
-    const int64_t grid = (int64_t)b.n_seq * b.max_q * b.n_heads * chunks;
-    if (grid > 0x7fffffffll) return comet_fail(ctx, COMET_ECAP, "%s: too many rows", what);
-    hipLaunchKernelGGL(scores_kernel, dim3((unsigned)grid), dim3(GT), 0, ctx->stream, p, chunks);
-    COMET_LAUNCH_CHECK(ctx, what);
-    return COMET_OK;
+    return launch_scores(ctx, what, p);
 }
 
 int comet_attention_values(comet_ctx* ctx, int party, const comet_kv_batch* batch, int d, int ldp, int64_t n_pages, int64_t ld,
@@ -187,7 +130,6 @@ int comet_attention_values(comet_ctx* ctx, int party, const comet_kv_batch* batc
                            const uint64_t* C_i, const uint64_t* M_i, uint64_t* Z_i, void* ws, size_t ws_bytes) {
     const char* what = "comet_attention_values";
     COMET_CHECK_CTX(ctx);
-    (void)ws; (void)ws_bytes;
     ProductParams p;
     const int rc = make_product(ctx, what, party, batch, d, ldp, n_pages, ld, frac_bits, E, A_i, f_pool, x_pool, C_i, M_i, Z_i, &p);
     if (rc != COMET_OK) return rc;
@@ -195,12 +137,7 @@ int comet_attention_values(comet_ctx* ctx, int party, const comet_kv_batch* batc
     if (b.n_tok == 0 || b.n_seq == 0 || b.max_q == 0) return COMET_OK;
     comet_device_guard guard(ctx);
     if (!guard.ok) return comet_fail(ctx, COMET_EDEVICE, "%s: cannot select device", what);
-    const int chunks = (d + GT - 1) / GT;
-    const int64_t grid = (int64_t)b.n_seq * b.max_q * b.n_heads * chunks;
-    if (grid > 0x7fffffffll) return comet_fail(ctx, COMET_ECAP, "%s: too many rows", what);
-    hipLaunchKernelGGL(values_kernel, dim3((unsigned)grid), dim3(GT), 0, ctx->stream, p, chunks);
-    COMET_LAUNCH_CHECK(ctx, what);
-    return COMET_OK;
+    return launch_values(ctx, what, p, ws, ws_bytes);
 }
 
 int comet_attention_weights(comet_ctx* ctx, int party, const comet_kv_batch* batch, int64_t ld, int frac_bits, uint64_t bias,

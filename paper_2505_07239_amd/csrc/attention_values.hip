@@ -1,0 +1,354 @@
+// Weights times cached values (comet_attention_values) on the int8 matrix cores:
+//     Z(r, c) = t(C(r, c) + sum_j E(r, j) X(j, c) + A(r, j) F(j, c)) - M(r, c).
+//
+// The contraction runs over the keys, in blocks of 64, for E X and A F in turn.  A lane loads the sixteen words of
+// its column in sixteen cached rows (consecutive lanes read consecutive columns) and of its row of weights, and splits and
+// transposes both in registers.  Two kernels:
+//   * values_few_kernel, up to 16 rows (a decoding step): bound by reading the cache once.  A wavefront has 16 rows x 64
+//     columns and every eighth block of keys; nothing is shared, so there is no barrier until the eight wavefronts of a
+//     workgroup add their sums up in LDS.
+//   * values_many_kernel: 16 RF rows x 128 columns.  A wavefront has 16 columns, whose cached words only it reads; the
+//     weights, which all of them need, are converted once by all threads into one of two LDS stages while the other is
+//     multiplied.  With at most 64 columns four wavefronts take E X and four A F.
+// Long sequences with few rows are cut into pieces, whose sums (of words, so that their order changes nothing)
+// values_finish_kernel adds up.
+#include "attention_tile.h"
+
+using namespace comet_attn;
+
+namespace {
+
+constexpr int NT = 512, W = NT / 64;
+constexpr int MAX_CHUNK = 8128;       // keys whose digit products an int32 plane can take: 2 * 8 * 8128 * 2^14 < 2^31
+constexpr int GROUPS16 = MAX_CHUNK / 16;
+
+// First slots of the groups of 16 keys (which lie in one page) from `first` on, in LDS.
+__device__ __forceinline__ void find_slots(int (&slots)[GROUPS16], const Batch& b, const Sequence& sq, int first, int end) {
+    for (int i = threadIdx.x; i < GROUPS16; i += NT) {
+        const int key = first + 16 * i;
+        slots[i] = key < end ? (int)sq.slot(b, key) : 0;
+    }
+}
+
+// The sixteen words of the lane's column in a block of 64 keys: key 8 j + 2 g + b is slot 2 j + b.
+// `q`: the block's first entry of `slots`; `lane_at`: byte offset of the lane's first row and column.
+__device__ __forceinline__ void load_column(const u64* pool, const int (&slots)[GROUPS16], int q, u32 row_bytes, u32 lane_at,
+                                            u64x2 (&w)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int slot = __builtin_amdgcn_readfirstlane(q + i < GROUPS16 ? slots[q + i] : 0);
+        const char* base = reinterpret_cast<const char*>(pool) + (size_t)slot * row_bytes;
+        u32 at = lane_at;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            w[2 * i + j].x = *reinterpret_cast<const u64*>(base + at);
+            w[2 * i + j].y = *reinterpret_cast<const u64*>(base + (at + row_bytes));
+            at += 8 * row_bytes;
+        }
+    }
+}
+
+// The sixteen words of the lane's row in a block of keys; nothing at or beyond `sees` counts.
+__device__ __forceinline__ void load_row(const u64* row, int key0, int sees, int g, u64x2 (&w)[8]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int key = key0 + 8 * j + 2 * g;
+        w[j] = u64x2{0, 0};
+        if (key < sees) {                                    // (rows are 16-byte aligned: ld is even)
+            w[j] = *reinterpret_cast<const u64x2*>(row + key);
+            if (key + 1 >= sees) w[j].y = 0;
+        }
+    }
+}
+
+__device__ __forceinline__ void write_word(const ProductParams& p, int row, int col, u64 sum) {
+    const size_t at = (size_t)row * p.d + col;
+    u64 z = rescale(p.party, p.C[at] + sum, p.frac);
+    if (p.M) z -= p.M[at];
+    p.Z[at] = z;
+}
+
+struct Piece {
+    int rt, cg, chunk;
+    __device__ __forceinline__ Piece(const ProductParams& p, int piece) {
+        chunk = piece % p.chunks;
+        piece /= p.chunks;
+        cg = piece % p.groups;
+        rt = p.tiles - 1 - piece / p.groups;                  // (the rows that see most come first)
+    }
+};
+
+// Sum of a piece: the result, or a partial sum.  A piece beyond what a row tile sees is not written, but for the first.
+__device__ __forceinline__ void put(const ProductParams& p, int chunk, int row, int col, u64 sum) {
+    if (p.part) p.part[((size_t)chunk * p.b.n_tok * p.b.n_heads + row) * p.d + col] = sum;
+    else write_word(p, row, col, sum);
+}
+
+__global__ __launch_bounds__(NT) void values_few_kernel(ProductParams p) {
+    constexpr int R = 16, CT = 4, COLS = 16 * CT;
+    __shared__ int slots[GROUPS16];
+    __shared__ RowTile<R> tile;
+    __shared__ u64 sums[R * COLS];
+    const Batch& b = p.b;
+    const Unit unit(b, p.tiles * p.groups * p.chunks);
+    if (!unit.live) return;
+    const Piece piece(p, unit.piece);
+    const Sequence sq(b, unit.s);
+    if (piece.rt * R >= sq.nq * b.group) return;
+    tile.fill(b, sq, unit.kvh, piece.rt * R);
+    __syncthreads();
+    int most, least;
+    tile.span(most, least);
+    const int first = piece.chunk * p.chunk;
+    const int end = most < first + p.chunk ? most : first + p.chunk;
+    if (first >= end && piece.chunk > 0) return;
+    find_slots(slots, b, sq, first, end);
+    for (int i = threadIdx.x; i < R * COLS; i += NT) sums[i] = 0;
+    __syncthreads();
+
+    const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int row = tile.row[r] < 0 ? 0 : tile.row[r], sees = tile.sees[r];
+    const u64* const e = p.E + (size_t)row * b.ld;
+    const u64* const a = p.A + (size_t)row * b.ld;
+    const u32 row_bytes = (u32)(b.n_kv_heads * p.ldp) * 8u;
+    u32 lane_at[CT];
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+        int col = piece.cg * COLS + c * 16 + r;
+        col = col < p.d ? col : p.d - 1;                      // (never written)
+        lane_at[c] = (u32)(2 * g) * row_bytes + (u32)(unit.kvh * p.ldp + col) * 8u;
+    }
+    v4i acc[CT][8];
+#pragma unroll
+    for (int c = 0; c < CT; ++c)
+#pragma unroll
+        for (int s = 0; s < 8; ++s) acc[c][s] = v4i{0, 0, 0, 0};
+    for (int key0 = first + 64 * wave; key0 < end; key0 += 64 * W) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            u64x2 w[8];
+            v4i x[8];
+            load_row(h ? a : e, key0, sees < end ? sees : end, g, w);
+            to_units(w, x);
+#pragma unroll
+            for (int c = 0; c < CT; ++c) {
+                v4i f[8];
+                load_column(h ? p.F : p.X, slots, (key0 - first) / 16, row_bytes, lane_at[c], w);
+                to_units(w, f);
+#pragma unroll
+                for (int t = 0; t < 8; ++t) mfma_digits(acc[c], x[t], f, t);
+            }
+        }
+    }
+#pragma unroll
+    for (int c = 0; c < CT; ++c)
+#pragma unroll
+        for (int e4 = 0; e4 < 4; ++e4) atomicAdd(&sums[(4 * g + e4) * COLS + c * 16 + r], word_of(acc[c], e4));
+    __syncthreads();
+    for (int i = threadIdx.x; i < R * COLS; i += NT) {
+        const int rr = i / COLS, col = piece.cg * COLS + i % COLS;
+        if (tile.row[rr] >= 0 && col < p.d) put(p, piece.chunk, tile.row[rr], col, sums[i]);
+    }
+}
+
+// COLW: wavefronts side by side along the columns; 4: the two halves of the workgroup take E X and A F.
+template <int RF, int COLW>
+__global__ __launch_bounds__(NT) void values_many_kernel(ProductParams p) {
+    constexpr int R = 16 * RF, COLS = 16 * COLW, HALF = R * 512, STAGE = 2 * HALF;
+    __shared__ __align__(16) unsigned char stage[2 * STAGE];
+    __shared__ int slots[GROUPS16];
+    __shared__ RowTile<R> tile;
+    const Batch& b = p.b;
+    const Unit unit(b, p.tiles * p.groups * p.chunks);
+    if (!unit.live) return;
+    const Piece piece(p, unit.piece);
+    const Sequence sq(b, unit.s);
+    if (piece.rt * R >= sq.nq * b.group) return;
+    tile.fill(b, sq, unit.kvh, piece.rt * R);
+    __syncthreads();
+    int most, least;
+    tile.span(most, least);
+    const int first = piece.chunk * p.chunk;
+    const int end = most < first + p.chunk ? most : first + p.chunk;
+    if (first >= end && piece.chunk > 0) return;
+    find_slots(slots, b, sq, first, end);
+    __syncthreads();
+
+    const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    // what this thread converts: its sixteen weights of row cr, of E (ch = 0) or A
+    const bool feeds = wave < 2 * RF;
+    const int ch = wave / RF, cr = (wave % RF) * 16 + r;
+    const int crow = feeds && tile.row[cr % R] >= 0 ? tile.row[cr % R] : 0;
+    int csees = feeds ? tile.sees[cr % R] : 0;
+    csees = csees < end ? csees : end;
+    const u64* const weights = (ch ? p.A : p.E) + (size_t)crow * b.ld;
+    unsigned char* const put_at = stage + ch * HALF + (g * R + cr) * 16;
+    // what it multiplies
+    const int cw = wave % COLW, h0 = COLW == 8 ? 0 : wave / COLW;
+    const u32 row_bytes = (u32)(b.n_kv_heads * p.ldp) * 8u;
+    const int col = piece.cg * COLS + cw * 16 + r;
+    const bool works = piece.cg * COLS + cw * 16 < p.d;
+    const u32 lane_at = (u32)(2 * g) * row_bytes + (u32)(unit.kvh * p.ldp + (col < p.d ? col : p.d - 1)) * 8u;
+    const unsigned char* const get_at = stage + (g * R + r) * 16;
+
+    v4i acc[RF][8];
+#pragma unroll
+    for (int i = 0; i < RF; ++i)
+#pragma unroll
+        for (int s = 0; s < 8; ++s) acc[i][s] = v4i{0, 0, 0, 0};
+    auto convert = [&](const u64x2 (&w)[8], int st) {
+        v4i f[8];
+        to_units(w, f);
+#pragma unroll
+        for (int t = 0; t < 8; ++t) *reinterpret_cast<v4i*>(put_at + st * STAGE + t * 4 * R * 16) = f[t];
+    };
+    auto multiply = [&](const v4i (&f)[8], const unsigned char* at) {
+#pragma unroll
+        for (int t = 0; t < 8; ++t)
+#pragma unroll
+            for (int i = 0; i < RF; ++i)
+                mfma_digits(acc[i], *reinterpret_cast<const v4i*>(at + (t * 4 * R + i * 16) * 16), f, t);
+    };
+    const int blocks = end > first ? (end - first + 63) / 64 : 0;
+    u64x2 w[8], v[8];
+    if (feeds && blocks > 0) {
+        load_row(weights, first, csees, g, w);
+        convert(w, 0);
+    }
+    if (works && blocks > 0) load_column(h0 ? p.F : p.X, slots, 0, row_bytes, lane_at, v);
+    for (int n = 0; n < blocks; ++n) {
+        __syncthreads();
+        const int st = n & 1;
+        const bool more = n + 1 < blocks;
+        if (COLW == 4) {
+            if (feeds && more) load_row(weights, first + 64 * (n + 1), csees, g, w);
+            if (works) {
+                v4i f[8];
+                to_units(v, f);
+                if (more) load_column(h0 ? p.F : p.X, slots, 4 * (n + 1), row_bytes, lane_at, v);
+                multiply(f, get_at + st * STAGE + h0 * HALF);
+            }
+        } else {
+            if (works) {
+                v4i f[8];
+                to_units(v, f);
+                load_column(p.F, slots, 4 * n, row_bytes, lane_at, v);
+                multiply(f, get_at + st * STAGE);
+            }
+            if (feeds && more) load_row(weights, first + 64 * (n + 1), csees, g, w);
+            if (works) {
+                v4i f[8];
+                to_units(v, f);
+                if (more) load_column(p.X, slots, 4 * (n + 1), row_bytes, lane_at, v);
+                multiply(f, get_at + st * STAGE + HALF);
+            }
+        }
+        if (feeds && more) convert(w, st ^ 1);
+    }
+    if (COLW == 4) {
+        // the halves of the workgroup meet in LDS
+        u64* const sums = reinterpret_cast<u64*>(stage);
+        __syncthreads();
+        if (h0 == 1 && works)
+#pragma unroll
+            for (int i = 0; i < RF; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sums[(16 * i + 4 * g + e) * COLS + cw * 16 + r] = word_of(acc[i], e);
+        __syncthreads();
+        if (h0 == 0 && works && col < p.d)
+#pragma unroll
+            for (int i = 0; i < RF; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int rr = 16 * i + 4 * g + e;
+                    if (tile.row[rr] >= 0) put(p, piece.chunk, tile.row[rr], col, word_of(acc[i], e) + sums[rr * COLS + cw * 16 + r]);
+                }
+    } else if (works && col < p.d) {
+#pragma unroll
+        for (int i = 0; i < RF; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int rr = 16 * i + 4 * g + e;
+                if (tile.row[rr] >= 0) put(p, piece.chunk, tile.row[rr], col, word_of(acc[i], e));
+            }
+    }
+}
+
+// Adds up the pieces of a row that have been written: those that begin before the last key it sees, and the first.
+__global__ __launch_bounds__(256) void values_finish_kernel(ProductParams p, int pieces) {
+    const Batch& b = p.b;
+    unsigned w = blockIdx.x;
+    const int piece = (int)(w % (unsigned)pieces); w /= (unsigned)pieces;
+    const int h = (int)(w % (unsigned)b.n_heads); w /= (unsigned)b.n_heads;
+    const int j = (int)(w % (unsigned)b.max_q);
+    const Sequence sq(b, (int)(w / (unsigned)b.max_q));
+    const int col = piece * 256 + threadIdx.x;
+    if (j >= sq.nq || col >= p.d) return;
+    const int row = (sq.q0 + j) * b.n_heads + h, sees = sq.sees(b, j, h);
+    const size_t all = (size_t)b.n_tok * b.n_heads * p.d;
+    const u64* from = p.part + (size_t)row * p.d + col;
+    u64 sum = from[0];
+    for (int c = 1; c * p.chunk < sees; ++c) sum += from[c * all];
+    write_word(p, row, col, sum);
+}
+
+// Pieces that the workspace of a call may hold: as many as a plane needs, and more while the partial sums of all rows
+// stay small (4 M words).
+int64_t max_chunks(int64_t m, int64_t ld, int64_t d) {
+    const int64_t needed = (ld + MAX_CHUNK - 1) / MAX_CHUNK;
+    int64_t n = m * d > 0 ? (4ll << 20) / (m * d) : 1;
+    if (n > 64) n = 64;
+    if (n > (ld + 255) / 256) n = (ld + 255) / 256;
+    return n < needed ? needed : n;
+}
+
+}  // namespace
+
+size_t comet_attn::values_workspace_bytes(int64_t m, int64_t ld, int64_t d) {
+    if (m < 0 || ld < 0 || d < 0 || d > MAX_D || ld > COMET_DIM_MAX || m > 0x7fffffffll) return 0;
+    const int64_t n = max_chunks(m, ld, d);
+    return n < 2 ? 0 : (size_t)n * m * d * 8;
+}
+
+int comet_attn::launch_values(comet_ctx* ctx, const char* what, ProductParams& p, void* ws, size_t ws_bytes) {
+    const Batch& b = p.b;
+    const int64_t n_rows = (int64_t)b.max_q * b.group, m = (int64_t)b.n_tok * b.n_heads;
+    const size_t need = values_workspace_bytes(m, b.ld, p.d);
+    if (need > 0 && (!ws || ws_bytes < need))
+        return comet_fail(ctx, COMET_EWORKSPACE, "%s: needs %zu bytes of workspace", what, need);
+    if (need > 0 && (reinterpret_cast<uintptr_t>(ws) & 255u) != 0)
+        return comet_fail(ctx, COMET_EALIGN, "%s: the workspace must be 256-byte aligned", what);
+    int R, cols, step;
+    void (*kern)(ProductParams);
+    if (n_rows <= 16) { kern = values_few_kernel; R = 16; cols = 64; step = 64 * W; }
+    else if (p.d <= 64) { kern = n_rows <= 32 ? values_many_kernel<2, 4> : values_many_kernel<4, 4>; R = n_rows <= 32 ? 32 : 64; cols = 64; step = 64; }
+    else { kern = n_rows <= 32 ? values_many_kernel<2, 8> : values_many_kernel<4, 8>; R = n_rows <= 32 ? 32 : 64; cols = 128; step = 64; }
+    p.tiles = (int)((n_rows + R - 1) / R);
+    p.groups = (p.d + cols - 1) / cols;
+    const int64_t units = (int64_t)b.n_seq * b.n_kv_heads * p.tiles * p.groups;
+    const int64_t cap = max_chunks(m, b.ld, p.d), needed = (b.kv_cap + MAX_CHUNK - 1) / MAX_CHUNK;
+    int64_t chunks = (4ll * ctx->num_cu + units - 1) / units;
+    const int64_t least = step < 256 ? 256 : step;            // keys a piece is worth
+    if (chunks > b.kv_cap / least) chunks = b.kv_cap / least;
+    if (chunks < needed) chunks = needed;
+    if (chunks > cap) chunks = cap;
+    if (chunks < 1) chunks = 1;
+    p.chunk = (int)(((b.kv_cap + chunks - 1) / chunks + 63) / 64 * 64);
+    if (p.chunk > MAX_CHUNK) p.chunk = MAX_CHUNK;
+    if (p.chunk < 64) p.chunk = 64;
+    p.chunks = b.kv_cap > 0 ? (b.kv_cap + p.chunk - 1) / p.chunk : 1;
+    p.part = p.chunks > 1 ? (u64*)ws : nullptr;
+    const int64_t grid = Unit::grid(b, (int64_t)p.tiles * p.groups * p.chunks);
+    const int pieces = (p.d + 255) / 256;
+    const int64_t finish = (int64_t)b.n_seq * b.max_q * b.n_heads * pieces;
+    if (grid > 0x7fffffffll || finish > 0x7fffffffll) return comet_fail(ctx, COMET_ECAP, "%s: too many rows", what);
+    hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(NT), 0, ctx->stream, p);
+    COMET_LAUNCH_CHECK(ctx, what);
+    if (p.part) {
+        hipLaunchKernelGGL(values_finish_kernel, dim3((unsigned)finish), dim3(256), 0, ctx->stream, p, pieces);
+        COMET_LAUNCH_CHECK(ctx, what);
+    }
+    return COMET_OK;
+}
