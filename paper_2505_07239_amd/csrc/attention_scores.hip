@@ -96,27 +96,33 @@ __global__ __launch_bounds__(NT) void scores_kernel(ProductParams p) {
             to_units(w, f);
             if (kb + 1 < blocks) load(off, kb + 1, w);
             else load(off_next, 0, w);
-            const unsigned char* at = mine + (size_t)kb * (R * 512);
-#pragma unroll
-            for (int t = 0; t < 8; ++t)
-#pragma unroll
-                for (int i = 0; i < RF; ++i)
-                    mfma_digits(acc[i], *reinterpret_cast<const v4i*>(at + (t * 4 * R + i * 16) * 16), f, t);
+            multiply_block<RF>(acc, f, mine + (size_t)kb * (R * 512));
         }
         off = off_next;
+        // the loads of several rows first: Z may be C or M, so the compiler would wait for every store before the next load
+        constexpr int BATCH = RF < 2 ? RF : 2;
         const int key = key0 + r;
 #pragma unroll
-        for (int i = 0; i < RF; ++i)
+        for (int i0 = 0; i0 < RF; i0 += BATCH) {
+            size_t at[BATCH][4];
+            bool live[BATCH][4];
+            u64 c[BATCH][4], m[BATCH][4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int rr = 16 * i + 4 * g + e;
-                if (key < tile.sees[rr]) {
-                    const size_t at = (size_t)tile.row[rr] * b.ld + key;
-                    u64 z = rescale(p.party, p.C[at] + word_of(acc[i], e), p.frac);
-                    if (p.M) z -= p.M[at];
-                    p.Z[at] = z;
+            for (int i = 0; i < BATCH; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int rr = 16 * (i0 + i) + 4 * g + e;
+                    live[i][e] = key < tile.sees[rr];
+                    at[i][e] = live[i][e] ? (size_t)tile.row[rr] * b.ld + key : 0;
+                    c[i][e] = p.C[at[i][e]];
+                    m[i][e] = p.M ? p.M[at[i][e]] : 0;
                 }
-            }
+#pragma unroll
+            for (int i = 0; i < BATCH; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (live[i][e]) p.Z[at[i][e]] = rescale(p.party, c[i][e] + word_of(acc[i0 + i], e), p.frac) - m[i][e];
+        }
     }
 }
 
@@ -134,11 +140,11 @@ int comet_attn::launch_scores(comet_ctx* ctx, const char* what, ProductParams& p
     else if (blocks <= 9) { kern = scores_kernel<1, 9, 512>; R = 16; W = 8; }
     else { kern = scores_kernel<1, 19, 1024>; R = 16; W = 16; }
     p.tiles = (int)((n_rows + R - 1) / R);
-    // Enough workgroups to fill the chip several times over (sequences differ in length), each with a few tiles of keys
-    // per wavefront at least, over which it reads its rows once.
-    const int64_t units = (int64_t)b.n_seq * b.n_kv_heads * p.tiles, wanted = 8ll * ctx->num_cu;
+    // Enough workgroups to fill the chip several times over (sequences differ in length), each with a tile of keys per
+    // wavefront at least.
+    const int64_t units = (int64_t)b.n_seq * b.n_kv_heads * p.tiles, wanted = (W == 4 ? 8ll : 2ll) * ctx->num_cu;
     int64_t chunks = (wanted + units - 1) / units;
-    const int64_t most = (b.kv_cap + 16 * W * 4 - 1) / (16 * W * 4);
+    const int64_t most = (b.kv_cap + 16 * W - 1) / (16 * W);
     if (chunks > most) chunks = most;
     if (chunks < 1) chunks = 1;
     p.chunk = (int)(((b.kv_cap + chunks - 1) / chunks + 16 * W - 1) / (16 * W) * (16 * W));

@@ -105,10 +105,27 @@ struct RowTile {
     }
 };
 
-__device__ __forceinline__ void mfma_digits(v4i (&acc)[8], const v4i& a, const v4i (&f)[8], int t) {
+// One block of 64 words: acc[i] += rows 16 i .. 16 i + 15 (digits in LDS, `at` the lane's unit of digit 0 of the first) times the
+// lane's column f.  The rows' units are read DEPTH ahead of their use, and the digits taken from both ends in turn, so that
+// every two units feed nine instructions.
+template <int RF>
+__device__ __forceinline__ void multiply_block(v4i (&acc)[RF][8], const v4i (&f)[8], const unsigned char* at) {
+    constexpr int N = 8 * RF, DEPTH = 4, R = 16 * RF;
+    auto digit = [](int n) { const int q = n / (2 * RF); return n & 1 ? 7 - q : q; };
+    auto sub = [](int n) { return n % (2 * RF) / 2; };
+    auto read = [&](int n) { return *reinterpret_cast<const v4i*>(at + (digit(n) * 4 * R + sub(n) * 16) * 16); };
+    v4i a[DEPTH];
 #pragma unroll
-    for (int u = 0; u < 8; ++u)
-        if (t + u < 8) acc[t + u] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a, f[u], acc[t + u], 0, 0, 0);
+    for (int n = 0; n < DEPTH; ++n) a[n] = read(n);
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        const int t = digit(n), i = sub(n);
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            if (t + u < 8) acc[i][t + u] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[n % DEPTH], f[u], acc[i][t + u], 0, 0, 0);
+        if (n + DEPTH < N) a[n % DEPTH] = read(n + DEPTH);
+        __builtin_amdgcn_sched_barrier(0);
+    }
 }
 
 int launch_scores(comet_ctx* ctx, const char* what, ProductParams& p);

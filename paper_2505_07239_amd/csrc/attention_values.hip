@@ -137,7 +137,10 @@ __global__ __launch_bounds__(NT) void values_few_kernel(ProductParams p) {
                 load_column(h ? p.F : p.X, slots, (key0 - first) / 16, row_bytes, lane_at[c], w);
                 to_units(w, f);
 #pragma unroll
-                for (int t = 0; t < 8; ++t) mfma_digits(acc[c], x[t], f, t);
+                for (int t = 0; t < 8; ++t)
+#pragma unroll
+                    for (int u = 0; t + u < 8; ++u)
+                        acc[c][t + u] = __builtin_amdgcn_mfma_i32_16x16x64_i8(x[t], f[u], acc[c][t + u], 0, 0, 0);
             }
         }
     }
@@ -204,13 +207,7 @@ __global__ __launch_bounds__(NT) void values_many_kernel(ProductParams p) {
 #pragma unroll
         for (int t = 0; t < 8; ++t) *reinterpret_cast<v4i*>(put_at + st * STAGE + t * 4 * R * 16) = f[t];
     };
-    auto multiply = [&](const v4i (&f)[8], const unsigned char* at) {
-#pragma unroll
-        for (int t = 0; t < 8; ++t)
-#pragma unroll
-            for (int i = 0; i < RF; ++i)
-                mfma_digits(acc[i], *reinterpret_cast<const v4i*>(at + (t * 4 * R + i * 16) * 16), f, t);
-    };
+    auto multiply = [&](const v4i (&f)[8], const unsigned char* at) { multiply_block<RF>(acc, f, at); };
     const int blocks = end > first ? (end - first + 63) / 64 : 0;
     u64x2 w[8], v[8];
     if (feeds && blocks > 0) {
