@@ -20,9 +20,9 @@ namespace {
 
 constexpr int NT = 512, W = NT / 64;
 constexpr int MAX_CHUNK = 8128;       // keys whose digit products an int32 plane can take: 2 * 8 * 8128 * 2^14 < 2^31
-constexpr int GROUPS16 = MAX_CHUNK / 16;
+constexpr int GROUPS16 = MAX_CHUNK / 16 + 4;
 
-// First slots of the groups of 16 keys (which lie in one page) from `first` on, in LDS.
+// First slots of the groups of 16 keys (which lie in one page) from `first` on, in LDS; slot 0 beyond the last.
 __device__ __forceinline__ void find_slots(int (&slots)[GROUPS16], const Batch& b, const Sequence& sq, int first, int end) {
     for (int i = threadIdx.x; i < GROUPS16; i += NT) {
         const int key = first + 16 * i;
@@ -30,34 +30,46 @@ __device__ __forceinline__ void find_slots(int (&slots)[GROUPS16], const Batch& 
     }
 }
 
-// The sixteen words of the lane's column in a block of 64 keys: key 8 j + 2 g + b is slot 2 j + b.
-// `q`: the block's first entry of `slots`; `lane_at`: byte offset of the lane's first row and column.
-__device__ __forceinline__ void load_column(const u64* pool, const int (&slots)[GROUPS16], int q, u32 row_bytes, u32 lane_at,
-                                            u64x2 (&w)[8]) {
+// The sixteen words of the lane's column in a block of 64 keys: key 8 j + 2 g + b is word 2 j + b.
+// `slots`: those of the block's four groups; `lane_at`: byte offset of the lane's first row and column.  Buffer loads, so
+// that a lane holds one offset for all of them.
+__device__ __forceinline__ void load_column(const u64* pool, const int* slots, u32 row_bytes, u32 lane_at, u64x2 (&w)[8]) {
+    const v4i four = *reinterpret_cast<const v4i*>(slots);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const int slot = __builtin_amdgcn_readfirstlane(q + i < GROUPS16 ? slots[q + i] : 0);
-        const char* base = reinterpret_cast<const char*>(pool) + (size_t)slot * row_bytes;
-        u32 at = lane_at;
+        const size_t at = (size_t)(u32)__builtin_amdgcn_readfirstlane(four[i]) * row_bytes;
+        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(reinterpret_cast<const char*>(pool) + at), 0, -1, 0x00027000);
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            w[2 * i + j].x = *reinterpret_cast<const u64*>(base + at);
-            w[2 * i + j].y = *reinterpret_cast<const u64*>(base + (at + row_bytes));
-            at += 8 * row_bytes;
+            w[2 * i + j].x = __builtin_bit_cast(u64, __builtin_amdgcn_raw_buffer_load_b64(rsrc, lane_at, 8 * j * row_bytes, 0));
+            w[2 * i + j].y = __builtin_bit_cast(u64, __builtin_amdgcn_raw_buffer_load_b64(rsrc, lane_at, (8 * j + 1) * row_bytes, 0));
         }
     }
 }
 
-// The sixteen words of the lane's row in a block of keys; nothing at or beyond `sees` counts.
-__device__ __forceinline__ void load_row(const u64* row, int key0, int sees, int g, u64x2 (&w)[8]) {
+// LDS accesses done, then meet the other wavefronts (loads from memory stay in flight).
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// The sixteen words of the lane's row in a block of keys (ld is even: rows are 16-byte aligned), and what does not count of
+// them made zero.  The second step uses the words, so it stays away from the loads.
+__device__ __forceinline__ void load_row(const u64* row, int key0, int ld, int g, u64x2 (&w)[8]) {
+    if (key0 + 64 <= ld) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = *reinterpret_cast<const u64x2*>(row + key0 + 8 * j + 2 * g);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int key = key0 + 8 * j + 2 * g;
+            w[j] = *reinterpret_cast<const u64x2*>(row + (key < ld ? key : ld - 2));
+        }
+    }
+}
+__device__ __forceinline__ void clear_unseen(u64x2 (&w)[8], int key0, int sees, int g) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         const int key = key0 + 8 * j + 2 * g;
-        w[j] = u64x2{0, 0};
-        if (key < sees) {                                    // (rows are 16-byte aligned: ld is even)
-            w[j] = *reinterpret_cast<const u64x2*>(row + key);
-            if (key + 1 >= sees) w[j].y = 0;
-        }
+        w[j].x = key < sees ? w[j].x : 0;
+        w[j].y = key + 1 < sees ? w[j].y : 0;
     }
 }
 
@@ -86,7 +98,7 @@ __device__ __forceinline__ void put(const ProductParams& p, int chunk, int row, 
 
 __global__ __launch_bounds__(NT) void values_few_kernel(ProductParams p) {
     constexpr int R = 16, CT = 4, COLS = 16 * CT;
-    __shared__ int slots[GROUPS16];
+    __shared__ __align__(16) int slots[GROUPS16];
     __shared__ RowTile<R> tile;
     __shared__ u64 sums[R * COLS];
     const Batch& b = p.b;
@@ -129,12 +141,13 @@ __global__ __launch_bounds__(NT) void values_few_kernel(ProductParams p) {
         for (int h = 0; h < 2; ++h) {
             u64x2 w[8];
             v4i x[8];
-            load_row(h ? a : e, key0, sees < end ? sees : end, g, w);
+            load_row(h ? a : e, key0, b.ld, g, w);
+            if (key0 + 64 > least) clear_unseen(w, key0, sees, g);
             to_units(w, x);
 #pragma unroll
             for (int c = 0; c < CT; ++c) {
                 v4i f[8];
-                load_column(h ? p.F : p.X, slots, (key0 - first) / 16, row_bytes, lane_at[c], w);
+                load_column(h ? p.F : p.X, slots + (key0 - first) / 16, row_bytes, lane_at[c], w);
                 to_units(w, f);
 #pragma unroll
                 for (int t = 0; t < 8; ++t)
@@ -160,7 +173,7 @@ template <int RF, int COLW>
 __global__ __launch_bounds__(NT) void values_many_kernel(ProductParams p) {
     constexpr int R = 16 * RF, COLS = 16 * COLW, HALF = R * 512, STAGE = 2 * HALF;
     __shared__ __align__(16) unsigned char stage[2 * STAGE];
-    __shared__ int slots[GROUPS16];
+    __shared__ __align__(16) int slots[GROUPS16];
     __shared__ RowTile<R> tile;
     const Batch& b = p.b;
     const Unit unit(b, p.tiles * p.groups * p.chunks);
@@ -183,11 +196,10 @@ __global__ __launch_bounds__(NT) void values_many_kernel(ProductParams p) {
     // what this thread converts: its sixteen weights of row cr, of E (ch = 0) or A
     const bool feeds = wave < 2 * RF;
     const int ch = wave / RF, cr = (wave % RF) * 16 + r;
-    const int crow = feeds && tile.row[cr % R] >= 0 ? tile.row[cr % R] : 0;
-    int csees = feeds ? tile.sees[cr % R] : 0;
-    csees = csees < end ? csees : end;
+    const int crow = feeds && tile.row[cr] >= 0 ? tile.row[cr] : 0;
+    const int csees = feeds ? tile.sees[cr] : 0;
     const u64* const weights = (ch ? p.A : p.E) + (size_t)crow * b.ld;
-    unsigned char* const put_at = stage + ch * HALF + (g * R + cr) * 16;
+    unsigned char* const put_at = stage + (ch & 1) * HALF + (g * R + cr) * 16;
     // what it multiplies
     const int cw = wave % COLW, h0 = COLW == 8 ? 0 : wave / COLW;
     const u32 row_bytes = (u32)(b.n_kv_heads * p.ldp) * 8u;
@@ -201,48 +213,55 @@ __global__ __launch_bounds__(NT) void values_many_kernel(ProductParams p) {
     for (int i = 0; i < RF; ++i)
 #pragma unroll
         for (int s = 0; s < 8; ++s) acc[i][s] = v4i{0, 0, 0, 0};
-    auto convert = [&](const u64x2 (&w)[8], int st) {
-        v4i f[8];
-        to_units(w, f);
-#pragma unroll
-        for (int t = 0; t < 8; ++t) *reinterpret_cast<v4i*>(put_at + st * STAGE + t * 4 * R * 16) = f[t];
-    };
-    auto multiply = [&](const v4i (&f)[8], const unsigned char* at) { multiply_block<RF>(acc, f, at); };
     const int blocks = end > first ? (end - first + 63) / 64 : 0;
-    u64x2 w[8], v[8];
-    if (feeds && blocks > 0) {
-        load_row(weights, first, csees, g, w);
-        convert(w, 0);
-    }
-    if (works && blocks > 0) load_column(h0 ? p.F : p.X, slots, 0, row_bytes, lane_at, v);
-    for (int n = 0; n < blocks; ++n) {
-        __syncthreads();
-        const int st = n & 1;
-        const bool more = n + 1 < blocks;
-        if (COLW == 4) {
-            if (feeds && more) load_row(weights, first + 64 * (n + 1), csees, g, w);
-            if (works) {
-                v4i f[8];
-                to_units(v, f);
-                if (more) load_column(h0 ? p.F : p.X, slots, 4 * (n + 1), row_bytes, lane_at, v);
-                multiply(f, get_at + st * STAGE + h0 * HALF);
+    // The two wavefronts of a SIMD are out of step: one converts its column behind the barrier, the other ahead of it, so
+    // that one multiplies while the other converts.
+    auto sweep = [&]<bool WORKS, bool FEEDS, bool LATE>() {
+        u64x2 w[8], v[8];
+        v4i f[8];
+        auto feed = [&](int key0, int st) {
+            v4i x[8];
+            if (key0 + 64 > least) clear_unseen(w, key0, csees, g);
+            to_units(w, x);
+#pragma unroll
+            for (int t = 0; t < 8; ++t) *reinterpret_cast<v4i*>(put_at + st * STAGE + t * 4 * R * 16) = x[t];
+        };
+        if constexpr (FEEDS) load_row(weights, first, b.ld, g, w);
+        if constexpr (WORKS) load_column(h0 ? p.F : p.X, slots, row_bytes, lane_at, v);
+        if constexpr (FEEDS) feed(first, 0);
+        if constexpr (WORKS && LATE) to_units(v, f);
+        for (int n = 0; n < blocks; ++n) {
+            lds_barrier();
+            const int next = n + 1 < blocks ? n + 1 : n;
+            const unsigned char* const from = get_at + (n & 1) * STAGE;
+            if constexpr (WORKS) {
+                if constexpr (!LATE) to_units(v, f);
+                __builtin_amdgcn_sched_barrier(0);
+                if constexpr (COLW == 8) {
+                    load_column(p.F, slots + 4 * n, row_bytes, lane_at, v);
+                    multiply_block<RF>(acc, f, from);
+                    to_units(v, f);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                load_column(h0 ? p.F : p.X, slots + 4 * next, row_bytes, lane_at, v);
             }
-        } else {
-            if (works) {
-                v4i f[8];
-                to_units(v, f);
-                load_column(p.F, slots, 4 * n, row_bytes, lane_at, v);
-                multiply(f, get_at + st * STAGE);
-            }
-            if (feeds && more) load_row(weights, first + 64 * (n + 1), csees, g, w);
-            if (works) {
-                v4i f[8];
-                to_units(v, f);
-                if (more) load_column(p.X, slots, 4 * (n + 1), row_bytes, lane_at, v);
-                multiply(f, get_at + st * STAGE + HALF);
-            }
+            if constexpr (FEEDS) load_row(weights, first + 64 * next, b.ld, g, w);
+            if constexpr (WORKS) multiply_block<RF>(acc, f, from + (COLW == 8 ? HALF : h0 * HALF));
+            if constexpr (FEEDS) feed(first + 64 * next, (n + 1) & 1);
+            if constexpr (WORKS && LATE) to_units(v, f);
         }
-        if (feeds && more) convert(w, st ^ 1);
+    };
+    if (blocks > 0) {
+        if (wave < 4) {                                       // (these feed, whatever RF is)
+            if (works) sweep.template operator()<true, true, false>();
+            else sweep.template operator()<false, true, false>();
+        } else if (feeds) {
+            if (works) sweep.template operator()<true, true, true>();
+            else sweep.template operator()<false, true, true>();
+        } else {
+            if (works) sweep.template operator()<true, false, true>();
+            else sweep.template operator()<false, false, true>();
+        }
     }
     if (COLW == 4) {
         // the halves of the workgroup meet in LDS
