@@ -110,7 +110,7 @@ struct RowTile {
 // every two units feed nine instructions.
 template <int RF>
 __device__ __forceinline__ void multiply_block(v4i (&acc)[RF][8], const v4i (&f)[8], const unsigned char* at) {
-    constexpr int N = 8 * RF, DEPTH = 3, R = 16 * RF;
+    constexpr int N = 8 * RF, DEPTH = 4, R = 16 * RF;
     auto digit = [](int n) { const int q = n / (2 * RF); return n & 1 ? 7 - q : q; };
     auto sub = [](int n) { return n % (2 * RF) / 2; };
     auto read = [&](int n) { return *reinterpret_cast<const v4i*>(at + (digit(n) * 4 * R + sub(n) * 16) * 16); };

@@ -14,6 +14,8 @@
 // values_finish_kernel adds up.
 #include "attention_tile.h"
 
+#include <type_traits>
+
 using namespace comet_attn;
 
 namespace {
@@ -50,24 +52,26 @@ __device__ __forceinline__ void load_column(const u64* pool, const int* slots, u
 // LDS accesses done, then meet the other wavefronts (loads from memory stay in flight).
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-// The sixteen words of the lane's row in a block of keys (ld is even: rows are 16-byte aligned), and what does not count of
-// them made zero.  The second step uses the words, so it stays away from the loads.
-__device__ __forceinline__ void load_row(const u64* row, int key0, int ld, int g, u64x2 (&w)[8]) {
+// Words 2 J .. 2 J + 2 N - 1 of the sixteen of the lane's row in a block of keys (ld is even: rows are 16-byte aligned), and
+// what does not count of them made zero.  The second step uses the words, so it stays away from the loads.
+template <int J, int N>
+__device__ __forceinline__ void load_row(const u64* row, int key0, int ld, int g, u64x2 (&w)[N]) {
     if (key0 + 64 <= ld) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) w[j] = *reinterpret_cast<const u64x2*>(row + key0 + 8 * j + 2 * g);
+        for (int j = 0; j < N; ++j) w[j] = *reinterpret_cast<const u64x2*>(row + key0 + 8 * (J + j) + 2 * g);
     } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int key = key0 + 8 * j + 2 * g;
+        for (int j = 0; j < N; ++j) {
+            const int key = key0 + 8 * (J + j) + 2 * g;
             w[j] = *reinterpret_cast<const u64x2*>(row + (key < ld ? key : ld - 2));
         }
     }
 }
-__device__ __forceinline__ void clear_unseen(u64x2 (&w)[8], int key0, int sees, int g) {
+template <int J, int N>
+__device__ __forceinline__ void clear_unseen(u64x2 (&w)[N], int key0, int sees, int g) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const int key = key0 + 8 * j + 2 * g;
+    for (int j = 0; j < N; ++j) {
+        const int key = key0 + 8 * (J + j) + 2 * g;
         w[j].x = key < sees ? w[j].x : 0;
         w[j].y = key + 1 < sees ? w[j].y : 0;
     }
@@ -141,8 +145,8 @@ __global__ __launch_bounds__(NT) void values_few_kernel(ProductParams p) {
         for (int h = 0; h < 2; ++h) {
             u64x2 w[8];
             v4i x[8];
-            load_row(h ? a : e, key0, b.ld, g, w);
-            if (key0 + 64 > least) clear_unseen(w, key0, sees, g);
+            load_row<0>(h ? a : e, key0, b.ld, g, w);
+            if (key0 + 64 > least) clear_unseen<0>(w, key0, sees, g);
             to_units(w, x);
 #pragma unroll
             for (int c = 0; c < CT; ++c) {
@@ -217,37 +221,69 @@ __global__ __launch_bounds__(NT) void values_many_kernel(ProductParams p) {
     // The two wavefronts of a SIMD are out of step: one converts its column behind the barrier, the other ahead of it, so
     // that one multiplies while the other converts.
     auto sweep = [&]<bool WORKS, bool FEEDS, bool LATE>() {
-        u64x2 w[8], v[8];
+        // (with eight column tiles half a unit of every digit at a time: the words on their way then fit beside the rest)
+        constexpr int WORDS = COLW == 8 ? 4 : 8;
+        u64x2 w[WORDS], v[8];
         v4i f[8];
-        auto feed = [&](int key0, int st) {
-            v4i x[8];
-            if (key0 + 64 > least) clear_unseen(w, key0, csees, g);
-            to_units(w, x);
-#pragma unroll
-            for (int t = 0; t < 8; ++t) *reinterpret_cast<v4i*>(put_at + st * STAGE + t * 4 * R * 16) = x[t];
+        auto request = [&]<int H>(std::integral_constant<int, H>, int key0) {
+            if constexpr (FEEDS) load_row<4 * H>(weights, key0, b.ld, g, w);
         };
-        if constexpr (FEEDS) load_row(weights, first, b.ld, g, w);
+        auto feed = [&]<int H>(std::integral_constant<int, H>, int key0, int st) {
+            if constexpr (FEEDS) {
+                if (key0 + 64 > least) clear_unseen<4 * H>(w, key0, csees, g);
+#pragma unroll
+                for (int o = 0; o < WORDS / 4; ++o) {
+                    u64 x[8], plane[8];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) { x[2 * i] = to_digits(w[4 * o + i].x); x[2 * i + 1] = to_digits(w[4 * o + i].y); }
+                    digits_to_planes(x, plane);
+#pragma unroll
+                    for (int t = 0; t < 8; ++t)
+                        *reinterpret_cast<u64*>(put_at + st * STAGE + t * 4 * R * 16 + 8 * (H + o)) = plane[t];
+                }
+            }
+        };
+        const std::integral_constant<int, 0> lower{};
+        const std::integral_constant<int, 1> upper{};
+        request(lower, first);
         if constexpr (WORKS) load_column(h0 ? p.F : p.X, slots, row_bytes, lane_at, v);
-        if constexpr (FEEDS) feed(first, 0);
+        feed(lower, first, 0);
+        if constexpr (COLW == 8) {
+            request(upper, first);
+            feed(upper, first, 0);
+        }
         if constexpr (WORKS && LATE) to_units(v, f);
         for (int n = 0; n < blocks; ++n) {
             lds_barrier();
-            const int next = n + 1 < blocks ? n + 1 : n;
+            const int next = n + 1 < blocks ? n + 1 : n, key0 = first + 64 * next, st = (n + 1) & 1;
             const unsigned char* const from = get_at + (n & 1) * STAGE;
-            if constexpr (WORKS) {
-                if constexpr (!LATE) to_units(v, f);
-                __builtin_amdgcn_sched_barrier(0);
-                if constexpr (COLW == 8) {
+            if constexpr (COLW == 8) {
+                if constexpr (WORKS) {
+                    if constexpr (!LATE) to_units(v, f);
+                    __builtin_amdgcn_sched_barrier(0);
                     load_column(p.F, slots + 4 * n, row_bytes, lane_at, v);
+                }
+                request(lower, key0);
+                if constexpr (WORKS) {
                     multiply_block<RF>(acc, f, from);
                     to_units(v, f);
                     __builtin_amdgcn_sched_barrier(0);
+                    load_column(p.X, slots + 4 * next, row_bytes, lane_at, v);
                 }
-                load_column(h0 ? p.F : p.X, slots + 4 * next, row_bytes, lane_at, v);
+                feed(lower, key0, st);
+                request(upper, key0);
+                if constexpr (WORKS) multiply_block<RF>(acc, f, from + HALF);
+                feed(upper, key0, st);
+            } else {
+                if constexpr (WORKS) {
+                    if constexpr (!LATE) to_units(v, f);
+                    __builtin_amdgcn_sched_barrier(0);
+                    load_column(h0 ? p.F : p.X, slots + 4 * next, row_bytes, lane_at, v);
+                }
+                request(lower, key0);
+                if constexpr (WORKS) multiply_block<RF>(acc, f, from + h0 * HALF);
+                feed(lower, key0, st);
             }
-            if constexpr (FEEDS) load_row(weights, first + 64 * next, b.ld, g, w);
-            if constexpr (WORKS) multiply_block<RF>(acc, f, from + (COLW == 8 ? HALF : h0 * HALF));
-            if constexpr (FEEDS) feed(first + 64 * next, (n + 1) & 1);
             if constexpr (WORKS && LATE) to_units(v, f);
         }
     };
