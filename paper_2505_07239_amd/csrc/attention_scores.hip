@@ -20,18 +20,18 @@ __global__ __launch_bounds__(NT) void scores_kernel(ProductParams p) {
     __shared__ __align__(16) unsigned char rows[KT * R * 512];
     __shared__ RowTile<R> tile;
     const Batch& b = p.b;
-    const Unit unit(b, p.tiles * p.chunks);
+    const Unit unit(b, p.tiles, p.chunks);
     if (!unit.live) return;
     const Sequence sq(b, unit.s);
     const int kvh = unit.kvh;
-    const int rt = p.tiles - 1 - unit.piece / p.chunks;       // (the rows that see most come first)
+    const int rt = p.tiles - 1 - unit.inner;       // (the rows that see most come first)
     const int r0 = rt * R;
     if (r0 >= sq.nq * b.group) return;
     tile.fill(b, sq, kvh, r0);
     __syncthreads();
     int most, least;
     tile.span(most, least);
-    const int first = (unit.piece % p.chunks) * p.chunk;
+    const int first = unit.chunk * p.chunk;
     const int end = most < first + p.chunk ? most : first + p.chunk;
     if (first >= end) return;
 
@@ -149,7 +149,7 @@ int comet_attn::launch_scores(comet_ctx* ctx, const char* what, ProductParams& p
     if (chunks < 1) chunks = 1;
     p.chunk = (int)(((b.kv_cap + chunks - 1) / chunks + 16 * W - 1) / (16 * W) * (16 * W));
     p.chunks = (b.kv_cap + p.chunk - 1) / p.chunk;
-    const int64_t grid = Unit::grid(b, (int64_t)p.tiles * p.chunks);
+    const int64_t grid = Unit::grid(b, p.tiles, p.chunks);
     if (grid > 0x7fffffffll) return comet_fail(ctx, COMET_ECAP, "%s: too many rows", what);
     hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(64 * W), 0, ctx->stream, p);
     COMET_LAUNCH_CHECK(ctx, what);

@@ -62,19 +62,23 @@ __device__ __forceinline__ u64 word_of(const v4i (&acc)[8], int e) {
     return (u64)lo + ((u64)hi << 32);
 }
 
-// The work of a workgroup: pairs (sequence, key head) are dealt to the eight XCDs one by one, and the pieces of a
-// pair, which read the same cached rows, follow each other on one XCD.
+// The work of a workgroup: a piece of the keys (chunk) of a (sequence, key head), and which of the `inner` units that read
+// the same cached rows it is.  Those follow each other on one of the eight XCDs, to which workgroups are dealt in turn.
 struct Unit {
-    int s, kvh, piece;
+    int s, kvh, chunk, inner;
     bool live;
-    __device__ __forceinline__ Unit(const Batch& b, int pieces) {
-        const unsigned q = blockIdx.x >> 3, pair = (q / (unsigned)pieces) * 8 + (blockIdx.x & 7);
-        piece = (int)(q % (unsigned)pieces);
+    __device__ __forceinline__ Unit(const Batch& b, int n_inner, int chunks) {
+        const unsigned q = blockIdx.x >> 3, group = (q / (unsigned)n_inner) * 8 + (blockIdx.x & 7);
+        const unsigned pair = group / (unsigned)chunks;
+        inner = (int)(q % (unsigned)n_inner);
+        chunk = (int)(group % (unsigned)chunks);
         live = pair < (unsigned)(b.n_seq * b.n_kv_heads);
         s = (int)(pair / (unsigned)b.n_kv_heads);
         kvh = (int)(pair % (unsigned)b.n_kv_heads);
     }
-    static int64_t grid(const Batch& b, int64_t pieces) { return ((int64_t)b.n_seq * b.n_kv_heads + 7) / 8 * 8 * pieces; }
+    static int64_t grid(const Batch& b, int64_t n_inner, int64_t chunks) {
+        return ((int64_t)b.n_seq * b.n_kv_heads * chunks + 7) / 8 * 8 * n_inner;
+    }
 };
 
 // Rows r0 .. r0 + R of a (sequence, key head): row number and keys seen of each, in LDS.  Row r is query head

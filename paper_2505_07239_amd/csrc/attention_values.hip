@@ -84,16 +84,6 @@ __device__ __forceinline__ void write_word(const ProductParams& p, int row, int 
     p.Z[at] = z;
 }
 
-struct Piece {
-    int rt, cg, chunk;
-    __device__ __forceinline__ Piece(const ProductParams& p, int piece) {
-        chunk = piece % p.chunks;
-        piece /= p.chunks;
-        cg = piece % p.groups;
-        rt = p.tiles - 1 - piece / p.groups;                  // (the rows that see most come first)
-    }
-};
-
 // Sum of a piece: the result, or a partial sum.  A piece beyond what a row tile sees is not written, but for the first.
 __device__ __forceinline__ void put(const ProductParams& p, int chunk, int row, int col, u64 sum) {
     if (p.part) p.part[((size_t)chunk * p.b.n_tok * p.b.n_heads + row) * p.d + col] = sum;
@@ -106,18 +96,19 @@ __global__ __launch_bounds__(NT) void values_few_kernel(ProductParams p) {
     __shared__ RowTile<R> tile;
     __shared__ u64 sums[R * COLS];
     const Batch& b = p.b;
-    const Unit unit(b, p.tiles * p.groups * p.chunks);
+    const Unit unit(b, p.tiles * p.groups, p.chunks);
     if (!unit.live) return;
-    const Piece piece(p, unit.piece);
+    const int rt = p.tiles - 1 - unit.inner / p.groups;       // (the rows that see most come first)
+    const int cg = unit.inner % p.groups;
     const Sequence sq(b, unit.s);
-    if (piece.rt * R >= sq.nq * b.group) return;
-    tile.fill(b, sq, unit.kvh, piece.rt * R);
+    if (rt * R >= sq.nq * b.group) return;
+    tile.fill(b, sq, unit.kvh, rt * R);
     __syncthreads();
     int most, least;
     tile.span(most, least);
-    const int first = piece.chunk * p.chunk;
+    const int first = unit.chunk * p.chunk;
     const int end = most < first + p.chunk ? most : first + p.chunk;
-    if (first >= end && piece.chunk > 0) return;
+    if (first >= end && unit.chunk > 0) return;
     find_slots(slots, b, sq, first, end);
     for (int i = threadIdx.x; i < R * COLS; i += NT) sums[i] = 0;
     __syncthreads();
@@ -131,7 +122,7 @@ __global__ __launch_bounds__(NT) void values_few_kernel(ProductParams p) {
     u32 lane_at[CT];
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
-        int col = piece.cg * COLS + c * 16 + r;
+        int col = cg * COLS + c * 16 + r;
         col = col < p.d ? col : p.d - 1;                      // (never written)
         lane_at[c] = (u32)(2 * g) * row_bytes + (u32)(unit.kvh * p.ldp + col) * 8u;
     }
@@ -167,8 +158,8 @@ __global__ __launch_bounds__(NT) void values_few_kernel(ProductParams p) {
         for (int e4 = 0; e4 < 4; ++e4) atomicAdd(&sums[(4 * g + e4) * COLS + c * 16 + r], word_of(acc[c], e4));
     __syncthreads();
     for (int i = threadIdx.x; i < R * COLS; i += NT) {
-        const int rr = i / COLS, col = piece.cg * COLS + i % COLS;
-        if (tile.row[rr] >= 0 && col < p.d) put(p, piece.chunk, tile.row[rr], col, sums[i]);
+        const int rr = i / COLS, col = cg * COLS + i % COLS;
+        if (tile.row[rr] >= 0 && col < p.d) put(p, unit.chunk, tile.row[rr], col, sums[i]);
     }
 }
 
@@ -180,18 +171,19 @@ __global__ __launch_bounds__(NT) void values_many_kernel(ProductParams p) {
     __shared__ __align__(16) int slots[GROUPS16];
     __shared__ RowTile<R> tile;
     const Batch& b = p.b;
-    const Unit unit(b, p.tiles * p.groups * p.chunks);
+    const Unit unit(b, p.tiles * p.groups, p.chunks);
     if (!unit.live) return;
-    const Piece piece(p, unit.piece);
+    const int rt = p.tiles - 1 - unit.inner / p.groups;       // (the rows that see most come first)
+    const int cg = unit.inner % p.groups;
     const Sequence sq(b, unit.s);
-    if (piece.rt * R >= sq.nq * b.group) return;
-    tile.fill(b, sq, unit.kvh, piece.rt * R);
+    if (rt * R >= sq.nq * b.group) return;
+    tile.fill(b, sq, unit.kvh, rt * R);
     __syncthreads();
     int most, least;
     tile.span(most, least);
-    const int first = piece.chunk * p.chunk;
+    const int first = unit.chunk * p.chunk;
     const int end = most < first + p.chunk ? most : first + p.chunk;
-    if (first >= end && piece.chunk > 0) return;
+    if (first >= end && unit.chunk > 0) return;
     find_slots(slots, b, sq, first, end);
     __syncthreads();
 
@@ -207,8 +199,8 @@ __global__ __launch_bounds__(NT) void values_many_kernel(ProductParams p) {
     // what it multiplies
     const int cw = wave % COLW, h0 = COLW == 8 ? 0 : wave / COLW;
     const u32 row_bytes = (u32)(b.n_kv_heads * p.ldp) * 8u;
-    const int col = piece.cg * COLS + cw * 16 + r;
-    const bool works = piece.cg * COLS + cw * 16 < p.d;
+    const int col = cg * COLS + cw * 16 + r;
+    const bool works = cg * COLS + cw * 16 < p.d;
     const u32 lane_at = (u32)(2 * g) * row_bytes + (u32)(unit.kvh * p.ldp + (col < p.d ? col : p.d - 1)) * 8u;
     const unsigned char* const get_at = stage + (g * R + r) * 16;
 
@@ -245,23 +237,28 @@ __global__ __launch_bounds__(NT) void values_many_kernel(ProductParams p) {
         };
         const std::integral_constant<int, 0> lower{};
         const std::integral_constant<int, 1> upper{};
-        request(lower, first);
-        if constexpr (WORKS) load_column(h0 ? p.F : p.X, slots, row_bytes, lane_at, v);
-        feed(lower, first, 0);
+        // Every second row tile begins in the middle: rows of weights are a few pages of memory apart, and workgroups that all
+        // read the same columns of them meet in the same few channels (512 rows of 4608 words: 784 us, and 600 with two
+        // beginnings; four and eight are no better, and cost hits in L2).
+        int blk = rt & 1 ? blocks / 2 : 0, key0 = first + 64 * blk;
+        request(lower, key0);
+        if constexpr (WORKS) load_column(h0 ? p.F : p.X, slots + 4 * blk, row_bytes, lane_at, v);
+        feed(lower, key0, 0);
         if constexpr (COLW == 8) {
-            request(upper, first);
-            feed(upper, first, 0);
+            request(upper, key0);
+            feed(upper, key0, 0);
         }
         if constexpr (WORKS && LATE) to_units(v, f);
         for (int n = 0; n < blocks; ++n) {
             lds_barrier();
-            const int next = n + 1 < blocks ? n + 1 : n, key0 = first + 64 * next, st = (n + 1) & 1;
+            const int next = blk + 1 < blocks ? blk + 1 : 0, st = (n + 1) & 1;
+            key0 = first + 64 * next;
             const unsigned char* const from = get_at + (n & 1) * STAGE;
             if constexpr (COLW == 8) {
                 if constexpr (WORKS) {
                     if constexpr (!LATE) to_units(v, f);
                     __builtin_amdgcn_sched_barrier(0);
-                    load_column(p.F, slots + 4 * n, row_bytes, lane_at, v);
+                    load_column(p.F, slots + 4 * blk, row_bytes, lane_at, v);
                 }
                 request(lower, key0);
                 if constexpr (WORKS) {
@@ -285,6 +282,7 @@ __global__ __launch_bounds__(NT) void values_many_kernel(ProductParams p) {
                 feed(lower, key0, st);
             }
             if constexpr (WORKS && LATE) to_units(v, f);
+            blk = next;
         }
     };
     if (blocks > 0) {
@@ -315,7 +313,7 @@ __global__ __launch_bounds__(NT) void values_many_kernel(ProductParams p) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int rr = 16 * i + 4 * g + e;
-                    if (tile.row[rr] >= 0) put(p, piece.chunk, tile.row[rr], col, word_of(acc[i], e) + sums[rr * COLS + cw * 16 + r]);
+                    if (tile.row[rr] >= 0) put(p, unit.chunk, tile.row[rr], col, word_of(acc[i], e) + sums[rr * COLS + cw * 16 + r]);
                 }
     } else if (works && col < p.d) {
 #pragma unroll
@@ -323,7 +321,7 @@ __global__ __launch_bounds__(NT) void values_many_kernel(ProductParams p) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int rr = 16 * i + 4 * g + e;
-                if (tile.row[rr] >= 0) put(p, piece.chunk, tile.row[rr], col, word_of(acc[i], e));
+                if (tile.row[rr] >= 0) put(p, unit.chunk, tile.row[rr], col, word_of(acc[i], e));
             }
     }
 }
@@ -379,20 +377,22 @@ int comet_attn::launch_values(comet_ctx* ctx, const char* what, ProductParams& p
     else { kern = n_rows <= 32 ? values_many_kernel<2, 8> : values_many_kernel<4, 8>; R = n_rows <= 32 ? 32 : 64; cols = 128; step = 64; }
     p.tiles = (int)((n_rows + R - 1) / R);
     p.groups = (p.d + cols - 1) / cols;
+    // Pieces of the keys: what the longest-working compute unit does, in steps of `step` keys, with two steps for the beginning
+    // and the end of a workgroup and four for the second launch, which more than one piece needs.
     const int64_t units = (int64_t)b.n_seq * b.n_kv_heads * p.tiles * p.groups;
     const int64_t cap = max_chunks(m, b.ld, p.d), needed = (b.kv_cap + MAX_CHUNK - 1) / MAX_CHUNK;
-    int64_t chunks = (4ll * ctx->num_cu + units - 1) / units;
-    const int64_t least = step < 256 ? 256 : step;            // keys a piece is worth
-    if (chunks > b.kv_cap / least) chunks = b.kv_cap / least;
-    if (chunks < needed) chunks = needed;
-    if (chunks > cap) chunks = cap;
-    if (chunks < 1) chunks = 1;
+    const int64_t steps = (b.kv_cap + step - 1) / step;
+    int64_t chunks = 1, best = INT64_MAX;
+    for (int64_t n = needed > 1 ? needed : 1; n <= cap && (n <= steps || n <= needed); ++n) {
+        const int64_t cost = (units * n + ctx->num_cu - 1) / ctx->num_cu * ((steps + n - 1) / n + 2) + (n > 1 ? 4 : 0);
+        if (cost < best) { best = cost; chunks = n; }
+    }
     p.chunk = (int)(((b.kv_cap + chunks - 1) / chunks + 63) / 64 * 64);
     if (p.chunk > MAX_CHUNK) p.chunk = MAX_CHUNK;
     if (p.chunk < 64) p.chunk = 64;
     p.chunks = b.kv_cap > 0 ? (b.kv_cap + p.chunk - 1) / p.chunk : 1;
     p.part = p.chunks > 1 ? (u64*)ws : nullptr;
-    const int64_t grid = Unit::grid(b, (int64_t)p.tiles * p.groups * p.chunks);
+    const int64_t grid = Unit::grid(b, (int64_t)p.tiles * p.groups, p.chunks);
     const int pieces = (p.d + 255) / 256;
     const int64_t finish = (int64_t)b.n_seq * b.max_q * b.n_heads * pieces;
     if (grid > 0x7fffffffll || finish > 0x7fffffffll) return comet_fail(ctx, COMET_ECAP, "%s: too many rows", what);
