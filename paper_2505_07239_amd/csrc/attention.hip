@@ -6,8 +6,6 @@ using namespace comet_attn;
 
 namespace {
 
-constexpr int GT = 256;
-
 struct WeightParams {
     Batch b;
     int party, frac;
@@ -21,34 +19,64 @@ struct WeightParams {
     u64* sums;
 };
 
-// One workgroup per row.
-__global__ __launch_bounds__(GT) void weights_kernel(WeightParams p) {
+// T threads per row, one pass: five words read and one written for each key, the sum kept in registers.  Bound by HBM, so
+// what counts is bytes on their way: a thread requests 2 U words of all operands before it uses the first (out may be one of
+// them, so the compiler could not look ahead by itself).
+template <int T>
+__global__ __launch_bounds__(T < 256 ? 256 : T) void weights_kernel(WeightParams p, int n_rows) {
+    constexpr int NT = T < 256 ? 256 : T, U = 2;
     const Batch& b = p.b;
-    unsigned w = blockIdx.x;
-    const int h = (int)(w % (unsigned)b.n_heads); w /= (unsigned)b.n_heads;
-    const int j = (int)(w % (unsigned)b.max_q);
-    const Sequence sq(b, (int)(w / (unsigned)b.max_q));
-    if (j >= sq.nq) return;
-    const int v = sq.sees(b, j, h);
-    const size_t row = (size_t)(sq.q0 + j) * b.n_heads + h;
+    const int place = (int)blockIdx.x * (NT / T) + (int)threadIdx.x / T, lane = (int)threadIdx.x % T;
+    const bool inside = place < n_rows;
+    const unsigned w = inside ? (unsigned)place : 0;
+    const int h = (int)(w % (unsigned)b.n_heads);
+    const int j = (int)(w / (unsigned)b.n_heads % (unsigned)b.max_q);
+    const Sequence sq(b, (int)(w / (unsigned)b.n_heads / (unsigned)b.max_q));
+    const bool live = inside && j < sq.nq;
+    const int v = live ? sq.sees(b, j, h) : 0;
+    const size_t row = (size_t)(sq.q0 + (live ? j : 0)) * b.n_heads + h, base = row * b.ld;
     u64 sum = 0;
-    for (int key = threadIdx.x; key < v; key += GT) {
-        const size_t at = row * b.ld + key;
-        const u64 u = p.d0[at] + (p.d1 ? p.d1[at] : 0) + p.bias;
-        u64 x = p.r2[at] + 2 * u * p.r[at];
-        if (p.party) x += u * u;
-        x = rescale(p.party, x, p.frac);
-        sum += x;
-        p.out[at] = p.m ? x - p.m[at] : x;
+    for (int key0 = 2 * lane; key0 < v; key0 += 2 * T * U) {
+        u64x2 u[U], u1[U], r[U], r2[U], m[U];
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            // (ld is even; beyond what the row sees its last pair again)
+            const int key = key0 + 2 * T * i;
+            const size_t at = base + (key < v ? key : (v - 1) & ~1);
+            u[i] = __builtin_nontemporal_load(reinterpret_cast<const u64x2*>(p.d0 + at));
+            u1[i] = p.d1 ? __builtin_nontemporal_load(reinterpret_cast<const u64x2*>(p.d1 + at)) : u64x2{0, 0};
+            r[i] = __builtin_nontemporal_load(reinterpret_cast<const u64x2*>(p.r + at));
+            r2[i] = __builtin_nontemporal_load(reinterpret_cast<const u64x2*>(p.r2 + at));
+            m[i] = p.m ? __builtin_nontemporal_load(reinterpret_cast<const u64x2*>(p.m + at)) : u64x2{0, 0};
+        }
+        auto square = [&](u64 x, u64 rr, u64 sq2) {
+            const u64 bias = x + p.bias;
+            return rescale(p.party, sq2 + bias * (p.party ? 2 * rr + bias : 2 * rr), p.frac);
+        };
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const int key = key0 + 2 * T * i;
+            const u64 x = square(u[i].x + u1[i].x, r[i].x, r2[i].x), y = square(u[i].y + u1[i].y, r[i].y, r2[i].y);
+            u64* const to = p.out + base + key;
+            if (key + 1 < v) {
+                sum += x + y;
+                __builtin_nontemporal_store(u64x2{x - m[i].x, y - m[i].y}, reinterpret_cast<u64x2*>(to));
+            } else if (key < v) {
+                sum += x;
+                *to = x - m[i].x;
+            }
+        }
     }
-    __shared__ u64 part[GT];
-    part[threadIdx.x] = sum;
-    __syncthreads();
-    for (int n = GT / 2; n > 0; n /= 2) {
-        if ((int)threadIdx.x < n) part[threadIdx.x] += part[threadIdx.x + n];
+#pragma unroll
+    for (int n = 32; n > 0; n /= 2) sum += __shfl_xor(sum, n);
+    if constexpr (T > 64) {
+        __shared__ u64 part[NT / 64];
+        if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = sum;
         __syncthreads();
+        sum = 0;
+        for (int i = 0; i < T / 64; ++i) sum += part[(threadIdx.x / T) * (T / 64) + i];
     }
-    if (threadIdx.x == 0) p.sums[row] = part[0];
+    if (live && lane == 0) p.sums[row] = sum;
 }
 
 // Checks of a batch; fills the device view.  COMET_OK with n_tok == 0 or n_seq == 0 means: nothing to do.
@@ -163,9 +191,15 @@ int comet_attention_weights(comet_ctx* ctx, int party, const comet_kv_batch* bat
     p.party = party; p.frac = frac_bits; p.bias = bias;
     p.d0 = (const u64*)d_0; p.d1 = (const u64*)d_1; p.r = (const u64*)r_i; p.r2 = (const u64*)r2_i; p.m = (const u64*)m_i;
     p.out = (u64*)out; p.sums = (u64*)sums;
-    const int64_t grid = (int64_t)b.n_seq * b.max_q * b.n_heads;
-    if (grid > 0x7fffffffll) return comet_fail(ctx, COMET_ECAP, "%s: too many rows", what);
-    hipLaunchKernelGGL(weights_kernel, dim3((unsigned)grid), dim3(GT), 0, ctx->stream, p);
+    const int64_t n_rows = (int64_t)b.n_seq * b.max_q * b.n_heads;
+    if (n_rows > 0x7fffffffll) return comet_fail(ctx, COMET_ECAP, "%s: too many rows", what);
+    // A wavefront per row where rows are short (prompts: many rows), a whole workgroup of sixteen where they are long and few.
+    if (b.kv_cap <= 1024)
+        hipLaunchKernelGGL(weights_kernel<64>, dim3((unsigned)((n_rows + 3) / 4)), dim3(256), 0, ctx->stream, p, (int)n_rows);
+    else if (b.kv_cap <= 4096)
+        hipLaunchKernelGGL(weights_kernel<256>, dim3((unsigned)n_rows), dim3(256), 0, ctx->stream, p, (int)n_rows);
+    else
+        hipLaunchKernelGGL(weights_kernel<1024>, dim3((unsigned)n_rows), dim3(1024), 0, ctx->stream, p, (int)n_rows);
     COMET_LAUNCH_CHECK(ctx, what);
     return COMET_OK;
 }

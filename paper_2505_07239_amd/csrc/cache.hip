@@ -12,40 +12,63 @@ template <int VEC> struct Word;
 template <> struct Word<1> { typedef u64 type; };
 template <> struct Word<2> { typedef u64x2 type; };
 
+// Everything here is read and written once: past the caches.
+template <class V>
+__device__ __forceinline__ V past(const u64* p, size_t i) { return __builtin_nontemporal_load(reinterpret_cast<const V*>(p) + i); }
+template <class V>
+__device__ __forceinline__ void put(u64* p, size_t i, V v) { __builtin_nontemporal_store(v, reinterpret_cast<V*>(p) + i); }
+
+// Which part of which row a workgroup's thread has: rows of many vectors are cut into pieces, narrow ones share a workgroup
+// (2^log lanes each).
+struct RowPart {
+    int t, first, step;
+    __device__ __forceinline__ RowPart(int pieces, int log) {
+        if (log < 8) {
+            t = (int)(blockIdx.x << (8 - log)) + ((int)threadIdx.x >> log);
+            first = (int)threadIdx.x & ((1 << log) - 1);
+            step = 1 << log;
+        } else {
+            t = (int)(blockIdx.x / (unsigned)pieces);
+            first = (int)(blockIdx.x % (unsigned)pieces) * GT + (int)threadIdx.x;
+            step = pieces * GT;
+        }
+    }
+};
+
 // One thread per VEC words of a row: F = d_0 + d_1 and X = b + party * F at the token's slot.
 template <int VEC>
 __global__ __launch_bounds__(GT) void cache_write_kernel(int party, const u64* __restrict__ d0, const u64* __restrict__ d1,
                                                          const u64* __restrict__ b, const int* __restrict__ slots,
-                                                         int nvec, u64* __restrict__ f_pool, u64* __restrict__ x_pool,
-                                                         int n_slots, int pieces) {
+                                                         int n_tok, int nvec, u64* __restrict__ f_pool,
+                                                         u64* __restrict__ x_pool, int n_slots, int pieces, int log) {
     typedef typename Word<VEC>::type V;
-    const int t = (int)(blockIdx.x / (unsigned)pieces), piece = (int)(blockIdx.x % (unsigned)pieces);
-    const int slot = slots[t];
+    const RowPart part(pieces, log);
+    if (part.t >= n_tok) return;
+    const int slot = slots[part.t];
     if (slot < 0 || slot >= n_slots) return;
-    const size_t from = (size_t)t * nvec, to = (size_t)slot * nvec;
-    for (int c = piece * GT + threadIdx.x; c < nvec; c += pieces * GT) {
-        const V f = reinterpret_cast<const V*>(d0)[from + c] + reinterpret_cast<const V*>(d1)[from + c];
-        const V x = reinterpret_cast<const V*>(b)[from + c];
-        reinterpret_cast<V*>(f_pool)[to + c] = f;
-        reinterpret_cast<V*>(x_pool)[to + c] = party ? x + f : x;
+    const size_t from = (size_t)part.t * nvec, to = (size_t)slot * nvec;
+    for (int c = part.first; c < nvec; c += part.step) {
+        const V f = past<V>(d0, from + c) + past<V>(d1, from + c), x = past<V>(b, from + c);
+        put<V>(f_pool, to + c, f);
+        put<V>(x_pool, to + c, party ? x + f : x);
     }
 }
 
 template <int VEC>
 __global__ __launch_bounds__(GT) void cache_read_kernel(int party, const u64* __restrict__ f_pool,
                                                         const u64* __restrict__ x_pool, const int* __restrict__ slots,
-                                                        int nvec, u64* __restrict__ e, u64* __restrict__ a, int n_slots,
-                                                        int pieces) {
+                                                        int n_tok, int nvec, u64* __restrict__ e, u64* __restrict__ a,
+                                                        int n_slots, int pieces, int log) {
     typedef typename Word<VEC>::type V;
-    const int t = (int)(blockIdx.x / (unsigned)pieces), piece = (int)(blockIdx.x % (unsigned)pieces);
-    const int slot = slots[t];
+    const RowPart part(pieces, log);
+    if (part.t >= n_tok) return;
+    const int slot = slots[part.t];
     if (slot < 0 || slot >= n_slots) return;
-    const size_t to = (size_t)t * nvec, from = (size_t)slot * nvec;
-    for (int c = piece * GT + threadIdx.x; c < nvec; c += pieces * GT) {
-        const V f = reinterpret_cast<const V*>(f_pool)[from + c];
-        const V x = reinterpret_cast<const V*>(x_pool)[from + c];
-        reinterpret_cast<V*>(e)[to + c] = f;
-        reinterpret_cast<V*>(a)[to + c] = party ? x - f : x;
+    const size_t to = (size_t)part.t * nvec, from = (size_t)slot * nvec;
+    for (int c = part.first; c < nvec; c += part.step) {
+        const V f = past<V>(f_pool, from + c), x = past<V>(x_pool, from + c);
+        put<V>(e, to + c, f);
+        put<V>(a, to + c, party ? x - f : x);
     }
 }
 
@@ -59,37 +82,61 @@ struct RotateParams {
     const u64* sin_t;
     const u64* m;
     u64* out;
-    int units;             // per token: heads x (pairs + unrotated words)
+    int units;             // per token: vectors of pairs and of words that are not rotated
 };
 
 __device__ __forceinline__ u64 rescale(int party, u64 v, int f) {
     return party == 0 ? (u64)((long long)v >> f) : (u64)0 - (u64)((long long)((u64)0 - v) >> f);
 }
 
-// One thread per pair, or per word that is not rotated.
+// One thread per VEC pairs, or VEC words that are not rotated.
+template <int VEC, bool INTERLEAVED>
 __global__ __launch_bounds__(GT) void rotate_kernel(RotateParams p, int pieces) {
+    typedef typename Word<VEC>::type V;
     const int t = (int)(blockIdx.x / (unsigned)pieces), piece = (int)(blockIdx.x % (unsigned)pieces);
-    const int per_head = p.head_dim - p.half;
-    const u64* x = p.x + (size_t)t * p.ldx;
+    const int pairs = p.half / VEC, per_head = pairs + (p.head_dim - 2 * p.half) / VEC;
+    const u64* const x = p.x + (size_t)t * p.ldx;
     const size_t row = (size_t)t * p.n_heads * p.head_dim;
+    const u64* const m = p.m ? p.m + row : nullptr;
+    u64* const out = p.out + row;
     long at = p.half ? p.pos[t] : 0;
     if (at < 0 || at >= p.n_pos) at = 0;
+    const u64* const cos_t = p.cos_t + (size_t)at * p.half;
+    const u64* const sin_t = p.sin_t + (size_t)at * p.half;
+    auto scaled = [&](V v, int f) {
+        if constexpr (VEC == 1) return rescale(p.party, v, f);
+        else return V{rescale(p.party, v.x, f), rescale(p.party, v.y, f)};
+    };
     for (int i = piece * GT + threadIdx.x; i < p.units; i += pieces * GT) {
         const int h = i / per_head, j = i - h * per_head;
         const int base = h * p.head_dim;
-        if (j < p.half) {
-            const int a = base + (p.interleaved ? 2 * j : j), b = base + (p.interleaved ? 2 * j + 1 : j + p.half);
-            const u64 c = p.cos_t[(size_t)at * p.half + j], s = p.sin_t[(size_t)at * p.half + j];
-            const u64 xa = rescale(p.party, x[a], p.shift), xb = rescale(p.party, x[b], p.shift);
-            u64 ya = rescale(p.party, xa * c - xb * s, p.frac), yb = rescale(p.party, xb * c + xa * s, p.frac);
-            if (p.m) { ya -= p.m[row + a]; yb -= p.m[row + b]; }
-            p.out[row + a] = ya;
-            p.out[row + b] = yb;
+        if (j < pairs) {
+            // the words p and q of VEC pairs, as vectors of consecutive words: (p, p + 1), (q, q + 1) or (p, q), (p', q')
+            const int a = base + (INTERLEAVED ? 2 * VEC * j : VEC * j), b = a + (INTERLEAVED ? VEC : p.half);
+            const V c = *reinterpret_cast<const V*>(cos_t + VEC * j), s = *reinterpret_cast<const V*>(sin_t + VEC * j);
+            V xa = scaled(past<V>(x + a, 0), p.shift), xb = scaled(past<V>(x + b, 0), p.shift);
+            if constexpr (INTERLEAVED && VEC == 2) {
+                const V ya = xa, yb = xb;
+                xa = V{ya.x, yb.x};
+                xb = V{ya.y, yb.y};
+            }
+            V ya = scaled(xa * c - xb * s, p.frac), yb = scaled(xb * c + xa * s, p.frac);
+            if constexpr (INTERLEAVED && VEC == 2) {
+                const V za = ya, zb = yb;
+                ya = V{za.x, zb.x};
+                yb = V{za.y, zb.y};
+            }
+            if (m) {
+                ya -= past<V>(m + a, 0);
+                yb -= past<V>(m + b, 0);
+            }
+            put<V>(out + a, 0, ya);
+            put<V>(out + b, 0, yb);
         } else {
-            const int a = base + j + p.half;
-            u64 y = rescale(p.party, x[a], p.shift);
-            if (p.m) y -= p.m[row + a];
-            p.out[row + a] = y;
+            const int a = base + 2 * p.half + VEC * (j - pairs);
+            V y = scaled(past<V>(x + a, 0), p.shift);
+            if (m) y -= past<V>(m + a, 0);
+            put<V>(out + a, 0, y);
         }
     }
 }
@@ -98,6 +145,16 @@ __global__ __launch_bounds__(GT) void rotate_kernel(RotateParams p, int pieces) 
 inline int row_pieces(int64_t n, int per_thread) {
     int64_t g = (n + (int64_t)GT * per_thread - 1) / ((int64_t)GT * per_thread);
     return (int)(g < 1 ? 1 : g > 64 ? 64 : g);
+}
+
+// lanes of a row, as a power of two: a whole workgroup (8) for rows of more than 128 vectors
+inline int row_log(int64_t n) {
+    int log = 3;
+    while (log < 8 && (1 << log) < n) ++log;
+    return log;
+}
+inline unsigned row_grid(int64_t n_tok, int pieces, int log) {
+    return (unsigned)(log < 8 ? (n_tok + (GT >> log) - 1) >> (8 - log) : n_tok * pieces);   // n_tok < 2^24, pieces <= 64
 }
 
 int check_rows(comet_ctx* ctx, const char* what, int party, const void* const (&ptrs)[5], const int32_t* slots, int64_t n_tok,
@@ -128,11 +185,11 @@ int comet_cache_write(comet_ctx* ctx, int party, const uint64_t* d_0, const uint
     comet_device_guard guard(ctx);
     if (!guard.ok) return comet_fail(ctx, COMET_EDEVICE, "%s: cannot select device", what);
     const bool vec = (width & 1) == 0;
-    const int nvec = (int)(vec ? width / 2 : width), pieces = row_pieces(nvec, 2);
-    const dim3 grid((unsigned)(n_tok * pieces));              // n_tok < 2^24, pieces <= 64
+    const int nvec = (int)(vec ? width / 2 : width), pieces = row_pieces(nvec, 2), log = row_log(nvec);
+    const dim3 grid(row_grid(n_tok, pieces, log));
     auto kern = vec ? cache_write_kernel<2> : cache_write_kernel<1>;
     hipLaunchKernelGGL(kern, grid, dim3(GT), 0, ctx->stream, party, (const u64*)d_0, (const u64*)d_1, (const u64*)b_i, slots,
-                       nvec, (u64*)f_pool, (u64*)x_pool, (int)n_slots, pieces);
+                       (int)n_tok, nvec, (u64*)f_pool, (u64*)x_pool, (int)n_slots, pieces, log);
     COMET_LAUNCH_CHECK(ctx, what);
     return COMET_OK;
 }
@@ -146,11 +203,11 @@ int comet_cache_read(comet_ctx* ctx, int party, const uint64_t* f_pool, const ui
     comet_device_guard guard(ctx);
     if (!guard.ok) return comet_fail(ctx, COMET_EDEVICE, "%s: cannot select device", what);
     const bool vec = (width & 1) == 0;
-    const int nvec = (int)(vec ? width / 2 : width), pieces = row_pieces(nvec, 2);
-    const dim3 grid((unsigned)(n_tok * pieces));
+    const int nvec = (int)(vec ? width / 2 : width), pieces = row_pieces(nvec, 2), log = row_log(nvec);
+    const dim3 grid(row_grid(n_tok, pieces, log));
     auto kern = vec ? cache_read_kernel<2> : cache_read_kernel<1>;
-    hipLaunchKernelGGL(kern, grid, dim3(GT), 0, ctx->stream, party, (const u64*)f_pool, (const u64*)x_pool, slots, nvec,
-                       (u64*)e, (u64*)a_i, (int)n_slots, pieces);
+    hipLaunchKernelGGL(kern, grid, dim3(GT), 0, ctx->stream, party, (const u64*)f_pool, (const u64*)x_pool, slots,
+                       (int)n_tok, nvec, (u64*)e, (u64*)a_i, (int)n_slots, pieces, log);
     COMET_LAUNCH_CHECK(ctx, what);
     return COMET_OK;
 }
@@ -182,9 +239,13 @@ int comet_rotate_share(comet_ctx* ctx, int party, const uint64_t* x_i, int64_t l
     p.shift = shift; p.frac = frac_bits; p.ldx = ldx; p.n_pos = n_pos;
     p.x = (const u64*)x_i; p.pos = positions; p.cos_t = (const u64*)cos_t; p.sin_t = (const u64*)sin_t;
     p.m = (const u64*)m_i; p.out = (u64*)out;
-    p.units = n_heads * (head_dim - p.half);
-    const int pieces = row_pieces(p.units, 2);
-    hipLaunchKernelGGL(rotate_kernel, dim3((unsigned)(n_tok * pieces)), dim3(GT), 0, ctx->stream, p, pieces);
+    // two words at a time where every vector of a head, of the table and of x_i starts on 16 bytes
+    const bool vec = (head_dim & 1) == 0 && (p.half & 1) == 0 && (ldx & 1) == 0 && comet_aligned16(x_i);
+    p.units = n_heads * (head_dim - p.half) / (vec ? 2 : 1);
+    const int pieces = row_pieces(p.units, 1);
+    auto kern = vec ? (p.interleaved ? rotate_kernel<2, true> : rotate_kernel<2, false>)
+                    : (p.interleaved ? rotate_kernel<1, true> : rotate_kernel<1, false>);
+    hipLaunchKernelGGL(kern, dim3((unsigned)(n_tok * pieces)), dim3(GT), 0, ctx->stream, p, pieces);
     COMET_LAUNCH_CHECK(ctx, what);
     return COMET_OK;
 }
