@@ -1,9 +1,9 @@
 // Queries times cached keys (comet_attention_scores) on the int8 matrix cores:
 //     Z(r, j) = t(C(r, j) + [E | A](r, :) . [X | F](j, :)) - M(r, j).
 //
-// A workgroup holds R = 16 RF rows in LDS, as digits, for the whole stacked contraction of 2 d words; behind
+// A workgroup holds R = 16 RF rows in LDS, as digits, for the whole stacked contraction (E and A, each filled up to whole blocks of 64 words); behind
 // the barrier that follows, its wavefronts are on their own.  Each takes every W-th tile of 16 keys: it loads its keys' words
-// straight into registers, a block of 64 ahead of their use, splits them into digits and transposes them there (no
+// straight into registers, a block of 64 words ahead of their use, splits them into digits and transposes them there (no
 // other wavefront of the workgroup wants them), and multiplies them with the rows' digits, read from LDS in operand
 // order.  So a cached word is fetched once per row tile, a query word once per workgroup, and while one
 // wavefront of a SIMD writes its tile out the other multiplies.
@@ -37,19 +37,19 @@ __global__ __launch_bounds__(NT) void scores_kernel(ProductParams p) {
 
     const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-    const int d = p.d, blocks = (2 * d + 63) / 64;
+    const int d = p.d, half = (d + 63) / 64, blocks = 2 * half;
 
     // the rows' digits: block kb, digit t, lane group g, row
     for (int i = wave; i < blocks * RF; i += W) {
         const int kb = i / RF, rr = (i % RF) * 16 + r;
         const int row = tile.row[rr];
+        const u64* const src = (kb < half ? p.E : p.A) + (size_t)(row < 0 ? 0 : row) * d;
         u64x2 w[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const int k = 64 * kb + 8 * j + 2 * g;
+            const int k = 64 * (kb < half ? kb : kb - half) + 8 * j + 2 * g;
             w[j] = u64x2{0, 0};
-            if (row >= 0 && k < 2 * d)
-                w[j] = *reinterpret_cast<const u64x2*>((k < d ? p.E + k : p.A + (k - d)) + (size_t)row * d);
+            if (row >= 0 && k < d) w[j] = *reinterpret_cast<const u64x2*>(src + k);
         }
         v4i f[8];
         to_units(w, f);
@@ -58,23 +58,20 @@ __global__ __launch_bounds__(NT) void scores_kernel(ProductParams p) {
     }
     __syncthreads();
 
-    // word offset of the lane's key of a tile (16 keys lie in one page)
-    const size_t stride = (size_t)b.n_kv_heads * p.ldp;
-    auto locate = [&](int key0) { return (sq.slot(b, key0) + r) * stride + (size_t)kvh * p.ldp; };
+    // A tile's 16 keys lie in one page: a uniform address, and one offset per lane.  Buffer loads that end with the page's 16
+    // rows: the last block may reach beyond d, where the rows' digits are zero, but never beyond the pool.
+    const u32 row_bytes = (u32)(b.n_kv_heads * p.ldp) * 8u, head_at = (u32)(kvh * p.ldp) * 8u;
+    const u32 lane_at = (u32)r * row_bytes + (u32)g * 16u, bytes = 16u * row_bytes - head_at;
+    auto locate = [&](int key0) {
+        return (size_t)(u32)__builtin_amdgcn_readfirstlane((int)sq.slot(b, key0)) * row_bytes + head_at;
+    };
     auto load = [&](size_t off, int kb, u64x2 (&w)[8]) {
-        const int k0 = 64 * kb;
-        if (k0 + 64 <= d || (k0 >= d && k0 + 64 <= 2 * d)) {
-            const u64* src = (k0 < d ? p.X + k0 : p.F + (k0 - d)) + off + 2 * g;
+        const u32 at = (u32)(kb < half ? kb : kb - half) * 512u;
+        const char* const pool = reinterpret_cast<const char*>(kb < half ? p.X : p.F) + off + at;
+        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(pool), 0, (int)(bytes - at), 0x00027000);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) w[j] = *reinterpret_cast<const u64x2*>(src + 8 * j);
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                int k = k0 + 8 * j + 2 * g;
-                k = k < 2 * d ? k : 2 * d - 2;               // (the rows' digits are zero there)
-                w[j] = *reinterpret_cast<const u64x2*>((k < d ? p.X + k : p.F + (k - d)) + off);
-            }
-        }
+        for (int j = 0; j < 8; ++j)
+            w[j] = __builtin_bit_cast(u64x2, __builtin_amdgcn_raw_buffer_load_b128(rsrc, lane_at + 64 * j, 0, 0));
     };
 
     int key0 = first + 16 * wave;
@@ -94,8 +91,9 @@ __global__ __launch_bounds__(NT) void scores_kernel(ProductParams p) {
         for (int kb = 0; kb < blocks; ++kb) {
             v4i f[8];
             to_units(w, f);
-            if (kb + 1 < blocks) load(off, kb + 1, w);
-            else load(off_next, 0, w);
+            __builtin_amdgcn_sched_barrier(0);
+            const bool last = kb + 1 == blocks;
+            load(last ? off_next : off, last ? 0 : kb + 1, w);
             multiply_block<RF>(acc, f, mine + (size_t)kb * (R * 512));
         }
         off = off_next;
@@ -114,14 +112,14 @@ __global__ __launch_bounds__(NT) void scores_kernel(ProductParams p) {
                     const int rr = 16 * (i0 + i) + 4 * g + e;
                     live[i][e] = key < tile.sees[rr];
                     at[i][e] = live[i][e] ? (size_t)tile.row[rr] * b.ld + key : 0;
-                    c[i][e] = p.C[at[i][e]];
-                    m[i][e] = p.M ? p.M[at[i][e]] : 0;
+                    c[i][e] = __builtin_nontemporal_load(p.C + at[i][e]);
+                    m[i][e] = p.M ? __builtin_nontemporal_load(p.M + at[i][e]) : 0;
                 }
 #pragma unroll
             for (int i = 0; i < BATCH; ++i)
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    if (live[i][e]) p.Z[at[i][e]] = rescale(p.party, c[i][e] + word_of(acc[i0 + i], e), p.frac) - m[i][e];
+                    if (live[i][e]) __builtin_nontemporal_store(rescale(p.party, c[i][e] + word_of(acc[i0 + i], e), p.frac) - m[i][e], p.Z + at[i][e]);
         }
     }
 }
@@ -130,15 +128,15 @@ __global__ __launch_bounds__(NT) void scores_kernel(ProductParams p) {
 
 int comet_attn::launch_scores(comet_ctx* ctx, const char* what, ProductParams& p) {
     const Batch& b = p.b;
-    const int blocks = (2 * p.d + 63) / 64;
+    const int blocks = (p.d + 63) / 64 * 2;
     const int64_t n_rows = (int64_t)b.max_q * b.group;
     int R, W;
     void (*kern)(ProductParams);
     if (n_rows > 32 && blocks <= 4) { kern = scores_kernel<4, 4, 512>; R = 64; W = 8; }
-    else if (n_rows > 16 && blocks <= 9) { kern = scores_kernel<2, 9, 512>; R = 32; W = 8; }
+    else if (n_rows > 16 && blocks <= 8) { kern = scores_kernel<2, 8, 512>; R = 32; W = 8; }
     else if (blocks <= 4) { kern = scores_kernel<1, 4, 256>; R = 16; W = 4; }
-    else if (blocks <= 9) { kern = scores_kernel<1, 9, 512>; R = 16; W = 8; }
-    else { kern = scores_kernel<1, 19, 1024>; R = 16; W = 16; }
+    else if (blocks <= 8) { kern = scores_kernel<1, 8, 512>; R = 16; W = 8; }
+    else { kern = scores_kernel<1, 18, 1024>; R = 16; W = 16; }
     p.tiles = (int)((n_rows + R - 1) / R);
     // Enough workgroups to fill the chip several times over (sequences differ in length), each with a tile of keys per
     // wavefront at least.

@@ -114,7 +114,7 @@ struct RowTile {
 // every two units feed nine instructions.
 template <int RF>
 __device__ __forceinline__ void multiply_block(v4i (&acc)[RF][8], const v4i (&f)[8], const unsigned char* at) {
-    constexpr int N = 8 * RF, DEPTH = 4, R = 16 * RF;
+    constexpr int N = 8 * RF, DEPTH = RF == 1 ? 2 : 4, R = 16 * RF;
     auto digit = [](int n) { const int q = n / (2 * RF); return n & 1 ? 7 - q : q; };
     auto sub = [](int n) { return n % (2 * RF) / 2; };
     auto read = [&](int n) { return *reinterpret_cast<const v4i*>(at + (digit(n) * 4 * R + sub(n) * 16) * 16); };
@@ -136,6 +136,6 @@ int launch_scores(comet_ctx* ctx, const char* what, ProductParams& p);
 int launch_values(comet_ctx* ctx, const char* what, ProductParams& p, void* ws, size_t ws_bytes);
 size_t values_workspace_bytes(int64_t m, int64_t ld, int64_t d);
 
-constexpr int MAX_D = 608;       // words of a cached row that a product contracts, or of a row of values
+constexpr int MAX_D = 576;       // words of a cached row that a product contracts, or of a row of values
 
 }  // namespace comet_attn

@@ -35,6 +35,7 @@ __device__ __forceinline__ void find_slots(int (&slots)[GROUPS16], const Batch& 
 // The sixteen words of the lane's column in a block of 64 keys: key 8 j + 2 g + b is word 2 j + b.
 // `slots`: those of the block's four groups; `lane_at`: byte offset of the lane's first row and column.  Buffer loads, so
 // that a lane holds one offset for all of them.
+template <int AUX = 0>
 __device__ __forceinline__ void load_column(const u64* pool, const int* slots, u32 row_bytes, u32 lane_at, u64x2 (&w)[8]) {
     const v4i four = *reinterpret_cast<const v4i*>(slots);
 #pragma unroll
@@ -43,8 +44,8 @@ __device__ __forceinline__ void load_column(const u64* pool, const int* slots, u
         const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(reinterpret_cast<const char*>(pool) + at), 0, -1, 0x00027000);
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            w[2 * i + j].x = __builtin_bit_cast(u64, __builtin_amdgcn_raw_buffer_load_b64(rsrc, lane_at, 8 * j * row_bytes, 0));
-            w[2 * i + j].y = __builtin_bit_cast(u64, __builtin_amdgcn_raw_buffer_load_b64(rsrc, lane_at, (8 * j + 1) * row_bytes, 0));
+            w[2 * i + j].x = __builtin_bit_cast(u64, __builtin_amdgcn_raw_buffer_load_b64(rsrc, lane_at, 8 * j * row_bytes, AUX));
+            w[2 * i + j].y = __builtin_bit_cast(u64, __builtin_amdgcn_raw_buffer_load_b64(rsrc, lane_at, (8 * j + 1) * row_bytes, AUX));
         }
     }
 }
@@ -142,7 +143,7 @@ __global__ __launch_bounds__(NT) void values_few_kernel(ProductParams p) {
 #pragma unroll
             for (int c = 0; c < CT; ++c) {
                 v4i f[8];
-                load_column(h ? p.F : p.X, slots + (key0 - first) / 16, row_bytes, lane_at[c], w);
+                load_column<2>(h ? p.F : p.X, slots + (key0 - first) / 16, row_bytes, lane_at[c], w);
                 to_units(w, f);
 #pragma unroll
                 for (int t = 0; t < 8; ++t)
