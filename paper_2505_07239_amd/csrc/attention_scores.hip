@@ -15,8 +15,8 @@ namespace {
 
 // KT: blocks of 64 words that fit the rows' place in LDS.  NT: threads.
 template <int RF, int KT, int NT>
-__global__ __launch_bounds__(NT) void scores_kernel(ProductParams p) {
-    constexpr int R = 16 * RF, W = NT / 64;
+__global__ __launch_bounds__(NT, RF == 1 && KT <= 8 ? 4 : 2) void scores_kernel(ProductParams p) {
+    constexpr int R = 16 * RF, W = NT / 64, AHEAD = KT > 8 ? 2 : 1;
     __shared__ __align__(16) unsigned char rows[KT * R * 512];
     __shared__ RowTile<R> tile;
     const Batch& b = p.b;
@@ -77,8 +77,9 @@ __global__ __launch_bounds__(NT) void scores_kernel(ProductParams p) {
     int key0 = first + 16 * wave;
     if (key0 >= end) return;
     size_t off = locate(key0);
-    u64x2 w[8];
-    load(off, 0, w);
+    u64x2 w[AHEAD][8];
+#pragma unroll
+    for (int n = 0; n < AHEAD; ++n) load(off, n, w[n]);       // (there are two blocks at least)
     const unsigned char* mine = rows + (g * R + r) * 16;
     for (; key0 < end; key0 += 16 * W) {
         const int next0 = key0 + 16 * W;
@@ -88,13 +89,17 @@ __global__ __launch_bounds__(NT) void scores_kernel(ProductParams p) {
         for (int i = 0; i < RF; ++i)
 #pragma unroll
             for (int s = 0; s < 8; ++s) acc[i][s] = v4i{0, 0, 0, 0};
-        for (int kb = 0; kb < blocks; ++kb) {
-            v4i f[8];
-            to_units(w, f);
-            __builtin_amdgcn_sched_barrier(0);
-            const bool last = kb + 1 == blocks;
-            load(last ? off_next : off, last ? 0 : kb + 1, w);
-            multiply_block<RF>(acc, f, mine + (size_t)kb * (R * 512));
+        for (int kb0 = 0; kb0 < blocks; kb0 += AHEAD) {       // (blocks is even, AHEAD one or two)
+#pragma unroll
+            for (int n = 0; n < AHEAD; ++n) {
+                v4i f[8];
+                to_units(w[n], f);
+                __builtin_amdgcn_sched_barrier(0);
+                const int kb = kb0 + n, then = kb + AHEAD;
+                const bool over = then >= blocks;
+                load(over ? off_next : off, over ? then - blocks : then, w[n]);
+                multiply_block<RF>(acc, f, mine + (size_t)kb * (R * 512));
+            }
         }
         off = off_next;
         // the loads of several rows first: Z may be C or M, so the compiler would wait for every store before the next load
@@ -136,11 +141,11 @@ int comet_attn::launch_scores(comet_ctx* ctx, const char* what, ProductParams& p
     else if (n_rows > 16 && blocks <= 8) { kern = scores_kernel<2, 8, 512>; R = 32; W = 8; }
     else if (blocks <= 4) { kern = scores_kernel<1, 4, 256>; R = 16; W = 4; }
     else if (blocks <= 8) { kern = scores_kernel<1, 8, 512>; R = 16; W = 8; }
-    else { kern = scores_kernel<1, 18, 1024>; R = 16; W = 16; }
+    else { kern = scores_kernel<1, 18, 768>; R = 16; W = 12; }
     p.tiles = (int)((n_rows + R - 1) / R);
     // Enough workgroups to fill the chip several times over (sequences differ in length), each with a tile of keys per
     // wavefront at least.
-    const int64_t units = (int64_t)b.n_seq * b.n_kv_heads * p.tiles, wanted = (W == 4 ? 8ll : 2ll) * ctx->num_cu;
+    const int64_t units = (int64_t)b.n_seq * b.n_kv_heads * p.tiles, wanted = (W == 4 ? 32ll : 2ll) * ctx->num_cu;
     int64_t chunks = (wanted + units - 1) / units;
     const int64_t most = (b.kv_cap + 16 * W - 1) / (16 * W);
     if (chunks > most) chunks = most;
