@@ -125,7 +125,8 @@ int make_product(comet_ctx* ctx, const char* what, int party, const comet_kv_bat
     p->E = (const u64*)E; p->A = (const u64*)A_i; p->F = (const u64*)f_pool; p->X = (const u64*)x_pool;
     p->C = (const u64*)C_i; p->M = (const u64*)M_i; p->Z = (u64*)Z_i;
     p->part = nullptr;
-    p->tiles = p->groups = p->chunks = p->chunk = 1;
+    p->far_rows = false;
+    p->tiles = p->groups = p->chunks = p->chunk = p->parts = 1;
     return COMET_OK;
 }
 

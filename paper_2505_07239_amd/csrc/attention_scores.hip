@@ -13,6 +13,58 @@ using namespace comet_attn;
 
 namespace {
 
+// A wavefront's tile: Z = t(C + sum) - M for the keys that its rows see.  All loads come before the first store: Z may be C or M,
+// so the compiler would keep them in order, and a load behind a store is not there before the store has been acknowledged
+// (the hardware counts both in order).  What a row does not see gets an offset outside the buffer, where loads give
+// zero and stores nothing.
+template <int RF>
+__device__ __forceinline__ void write_out(const ProductParams& p, const RowTile<16 * RF>& tile, const v4i (&acc)[RF][8], int key0,
+                                          int lane) {
+    const int r = lane & 15, g = lane >> 4, key = key0 + r;
+    if (!p.far_rows) {
+        const int row0 = __builtin_amdgcn_readfirstlane(tile.row0);
+        const size_t base = (size_t)row0 * p.b.ld + key0;
+        const auto at = [&](const u64* q) {
+            return __builtin_amdgcn_make_buffer_rsrc(const_cast<u64*>(q + base), 0, 0x7fffffff, 0x00027000);
+        };
+        const auto rc = at(p.C), rm = at(p.M ? p.M : p.C), rz = at(p.Z);
+        u32 off[RF][4];
+        u64 c[RF][4], m[RF][4];
+#pragma unroll
+        for (int i = 0; i < RF; ++i) {
+            const v4i row = *reinterpret_cast<const v4i*>(tile.row + 16 * i + 4 * g);
+            const v4i sees = *reinterpret_cast<const v4i*>(tile.sees + 16 * i + 4 * g);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                off[i][e] = key < sees[e] ? (u32)(row[e] - row0) * ((u32)p.b.ld * 8u) + (u32)r * 8u : 0xffffffffu;
+                c[i][e] = __builtin_bit_cast(u64, __builtin_amdgcn_raw_buffer_load_b64(rc, off[i][e], 0, 2));
+                m[i][e] = p.M ? __builtin_bit_cast(u64, __builtin_amdgcn_raw_buffer_load_b64(rm, off[i][e], 0, 2)) : 0;
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < RF; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const u64 z = rescale(p.party, c[i][e] + word_of(acc[i], e), p.frac) - m[i][e];
+                __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(v2u, z), rz, off[i][e], 0, 2);
+            }
+    } else {
+        // rows of a tile 2 GB apart or more
+#pragma unroll
+        for (int i = 0; i < RF; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int rr = 16 * i + 4 * g + e;
+                if (key < tile.sees[rr]) {
+                    const size_t at = (size_t)tile.row[rr] * p.b.ld + key;
+                    const u64 m = p.M ? p.M[at] : 0;
+                    p.Z[at] = rescale(p.party, p.C[at] + word_of(acc[i], e), p.frac) - m;
+                }
+            }
+    }
+}
+
 // KT: blocks of 64 words that fit the rows' place in LDS.  NT: threads.
 template <int RF, int KT, int NT>
 __global__ __launch_bounds__(NT, RF == 1 && KT <= 8 ? 4 : 2) void scores_kernel(ProductParams p) {
@@ -20,7 +72,7 @@ __global__ __launch_bounds__(NT, RF == 1 && KT <= 8 ? 4 : 2) void scores_kernel(
     __shared__ __align__(16) unsigned char rows[KT * R * 512];
     __shared__ RowTile<R> tile;
     const Batch& b = p.b;
-    const Unit unit(b, p.tiles, p.chunks);
+    const Unit unit(b, p.tiles, p.chunks, p.parts);
     if (!unit.live) return;
     const Sequence sq(b, unit.s);
     const int kvh = unit.kvh;
@@ -39,25 +91,6 @@ __global__ __launch_bounds__(NT, RF == 1 && KT <= 8 ? 4 : 2) void scores_kernel(
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int d = p.d, half = (d + 63) / 64, blocks = 2 * half;
 
-    // the rows' digits: block kb, digit t, lane group g, row
-    for (int i = wave; i < blocks * RF; i += W) {
-        const int kb = i / RF, rr = (i % RF) * 16 + r;
-        const int row = tile.row[rr];
-        const u64* const src = (kb < half ? p.E : p.A) + (size_t)(row < 0 ? 0 : row) * d;
-        u64x2 w[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int k = 64 * (kb < half ? kb : kb - half) + 8 * j + 2 * g;
-            w[j] = u64x2{0, 0};
-            if (row >= 0 && k < d) w[j] = *reinterpret_cast<const u64x2*>(src + k);
-        }
-        v4i f[8];
-        to_units(w, f);
-#pragma unroll
-        for (int t = 0; t < 8; ++t) *reinterpret_cast<v4i*>(rows + ((size_t)((kb * 8 + t) * 4 + g) * R + rr) * 16) = f[t];
-    }
-    __syncthreads();
-
     // A tile's 16 keys lie in one page: a uniform address, and one offset per lane.  Buffer loads that end with the page's 16
     // rows: the last block may reach beyond d, where the rows' digits are zero, but never beyond the pool.
     const u32 row_bytes = (u32)(b.n_kv_heads * p.ldp) * 8u, head_at = (u32)(kvh * p.ldp) * 8u;
@@ -65,21 +98,49 @@ __global__ __launch_bounds__(NT, RF == 1 && KT <= 8 ? 4 : 2) void scores_kernel(
     auto locate = [&](int key0) {
         return (size_t)(u32)__builtin_amdgcn_readfirstlane((int)sq.slot(b, key0)) * row_bytes + head_at;
     };
-    auto load = [&](size_t off, int kb, u64x2 (&w)[8]) {
+    auto block_at = [&](size_t off, int kb) {
         const u32 at = (u32)(kb < half ? kb : kb - half) * 512u;
         const char* const pool = reinterpret_cast<const char*>(kb < half ? p.X : p.F) + off + at;
-        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(pool), 0, (int)(bytes - at), 0x00027000);
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(pool), 0, (int)(bytes - at), 0x00027000);
+    };
+    auto load = [&](size_t off, int kb, u64x2 (&w)[8]) {
+        const auto rsrc = block_at(off, kb);
 #pragma unroll
         for (int j = 0; j < 8; ++j)
             w[j] = __builtin_bit_cast(u64x2, __builtin_amdgcn_raw_buffer_load_b128(rsrc, lane_at + 64 * j, 0, 0));
     };
 
     int key0 = first + 16 * wave;
-    if (key0 >= end) return;
-    size_t off = locate(key0);
+    size_t off = key0 < end ? locate(key0) : 0;
     u64x2 w[AHEAD][8];
 #pragma unroll
     for (int n = 0; n < AHEAD; ++n) load(off, n, w[n]);       // (there are two blocks at least)
+    // the rows' digits: block kb, digit t, lane group g, row
+    auto fetch_rows = [&](int i, u64x2 (&w)[8]) {
+        const int kb = i / RF, row = tile.row[(i % RF) * 16 + r];
+        const u64* const src = (kb < half ? p.E : p.A) + (size_t)(row < 0 ? 0 : row) * d;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int k = 64 * (kb < half ? kb : kb - half) + 8 * j + 2 * g;
+            w[j] = u64x2{0, 0};
+            if (row >= 0 && k < d) w[j] = *reinterpret_cast<const u64x2*>(src + k);
+        }
+    };
+    {
+        u64x2 now[8], next[8];
+        if (wave < blocks * RF) fetch_rows(wave, now);
+        for (int i = wave; i < blocks * RF; i += W) {
+            if (i + W < blocks * RF) fetch_rows(i + W, next);
+            v4i f[8];
+            to_units(now, f);
+            unsigned char* const to = rows + ((size_t)(i / RF * 32 + g) * R + (i % RF) * 16 + r) * 16;
+#pragma unroll
+            for (int t = 0; t < 8; ++t) *reinterpret_cast<v4i*>(to + t * 4 * R * 16) = f[t];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) now[j] = next[j];
+        }
+    }
+    __syncthreads();
     const unsigned char* mine = rows + (g * R + r) * 16;
     for (; key0 < end; key0 += 16 * W) {
         const int next0 = key0 + 16 * W;
@@ -102,31 +163,80 @@ __global__ __launch_bounds__(NT, RF == 1 && KT <= 8 ? 4 : 2) void scores_kernel(
             }
         }
         off = off_next;
-        // the loads of several rows first: Z may be C or M, so the compiler would wait for every store before the next load
-        constexpr int BATCH = RF < 2 ? RF : 2;
-        const int key = key0 + r;
-#pragma unroll
-        for (int i0 = 0; i0 < RF; i0 += BATCH) {
-            size_t at[BATCH][4];
-            bool live[BATCH][4];
-            u64 c[BATCH][4], m[BATCH][4];
-#pragma unroll
-            for (int i = 0; i < BATCH; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int rr = 16 * (i0 + i) + 4 * g + e;
-                    live[i][e] = key < tile.sees[rr];
-                    at[i][e] = live[i][e] ? (size_t)tile.row[rr] * b.ld + key : 0;
-                    c[i][e] = __builtin_nontemporal_load(p.C + at[i][e]);
-                    m[i][e] = p.M ? __builtin_nontemporal_load(p.M + at[i][e]) : 0;
-                }
-#pragma unroll
-            for (int i = 0; i < BATCH; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (live[i][e]) __builtin_nontemporal_store(rescale(p.party, c[i][e] + word_of(acc[i0 + i], e), p.frac) - m[i][e], p.Z + at[i][e]);
-        }
+        write_out<RF>(p, tile, acc, key0, lane);
     }
+}
+
+// What a wavefront of scores_many_kernel reads: its row of E or A, its 16 keys.
+struct Source {
+    const u64* rows;
+    const char *X, *F;             // the keys' rows of the head
+    int d, g;
+    u32 lane_at, bytes;
+    template <int J, int N>
+    __device__ __forceinline__ void row(int blk, u64x2 (&w)[N]) const { load_row<J>(rows, 64 * blk, d, g, w); }
+    template <int J, int N>
+    __device__ __forceinline__ void clear(int blk, u64x2 (&w)[N]) const {
+        if (64 * blk + 64 > d) clear_beyond<J>(w, 64 * blk, d, g);
+    }
+    __device__ __forceinline__ void column(int h, int blk, u64x2 (&v)[8]) const {
+        const u32 at = (u32)blk * 512u;
+        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>((h ? F : X) + at), 0, (int)(bytes - at), 0x00027000);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            v[j] = __builtin_bit_cast(u64x2, __builtin_amdgcn_raw_buffer_load_b128(rsrc, lane_at + 64 * j, 0, 0));
+    }
+};
+
+// Rows whose digits do not fit LDS: 16 RF rows x 128 keys, the contraction streamed (sweep_blocks).
+template <int RF>
+__global__ __launch_bounds__(512) void scores_many_kernel(ProductParams p) {
+    constexpr int R = 16 * RF, HALF = R * 512;
+    __shared__ __align__(16) unsigned char stage[4 * HALF];
+    __shared__ RowTile<R> tile;
+    const Batch& b = p.b;
+    const Unit unit(b, p.tiles, p.chunks, p.parts);
+    if (!unit.live) return;
+    const Sequence sq(b, unit.s);
+    const int r0 = (p.tiles - 1 - unit.inner) * R;
+    if (r0 >= sq.nq * b.group) return;
+    tile.fill(b, sq, unit.kvh, r0);
+    __syncthreads();
+    int most, least;
+    tile.span(most, least);
+    if (unit.chunk * p.chunk >= most) return;
+
+    const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int key0 = unit.chunk * p.chunk + 16 * wave;        // (a chunk is 128 keys)
+    const bool works = key0 < most, feeds = wave < 2 * RF;
+    const int ch = (wave / RF) & 1, cr = (wave % RF) * 16 + r, row = tile.row[cr] < 0 ? 0 : tile.row[cr];
+    const u32 row_bytes = (u32)(b.n_kv_heads * p.ldp) * 8u, head_at = (u32)(unit.kvh * p.ldp) * 8u;
+    const size_t off = works ? (size_t)(u32)__builtin_amdgcn_readfirstlane((int)sq.slot(b, key0)) * row_bytes + head_at : 0;
+    const Source src = {(ch ? p.A : p.E) + (size_t)row * p.d, reinterpret_cast<const char*>(p.X) + off,
+                        reinterpret_cast<const char*>(p.F) + off, p.d, g, (u32)r * row_bytes + (u32)g * 16u,
+                        16u * row_bytes - head_at};
+    unsigned char* const put_at = stage + ch * HALF + (g * R + cr) * 16;
+    const unsigned char* const get_at = stage + (g * R + r) * 16;
+    v4i acc[RF][8];
+#pragma unroll
+    for (int i = 0; i < RF; ++i)
+#pragma unroll
+        for (int s = 0; s < 8; ++s) acc[i][s] = v4i{0, 0, 0, 0};
+    auto sweep = [&]<bool WORKS, bool FEEDS, bool LATE>() {
+        sweep_blocks<RF, 2, WORKS, FEEDS, LATE>(acc, src, (p.d + 63) / 64, 0, 0, put_at, get_at);
+    };
+    if (wave < 4) {                                           // (these feed, whatever RF is)
+        if (works) sweep.template operator()<true, true, false>();
+        else sweep.template operator()<false, true, false>();
+    } else if (feeds) {
+        if (works) sweep.template operator()<true, true, true>();
+        else sweep.template operator()<false, true, true>();
+    } else {
+        if (works) sweep.template operator()<true, false, true>();
+        else sweep.template operator()<false, false, true>();
+    }
+    if (works) write_out<RF>(p, tile, acc, key0, lane);
 }
 
 }  // namespace
@@ -137,22 +247,33 @@ int comet_attn::launch_scores(comet_ctx* ctx, const char* what, ProductParams& p
     const int64_t n_rows = (int64_t)b.max_q * b.group;
     int R, W;
     void (*kern)(ProductParams);
-    if (n_rows > 32 && blocks <= 4) { kern = scores_kernel<4, 4, 512>; R = 64; W = 8; }
+    const int64_t pairs = (int64_t)b.n_seq * b.n_kv_heads;
+    // The streamed kernel reads keys once for 64 rows instead of 16, but starts slowly: for long contractions, when there are
+    // workgroups for every compute unit (d = 576, 37 tokens of 64 heads over 2037 keys: 807 -> 270 us; one token of 64 heads of
+    // 4 sequences: 64 us here and 88 streamed; d = 192: 117 here and 173).
+    const bool many = n_rows > 16 && blocks > 8 && pairs * ((n_rows + 63) / 64) * ((b.kv_cap + 127) / 128) >= ctx->num_cu;
+    if (many) { kern = n_rows > 32 ? scores_many_kernel<4> : scores_many_kernel<2>; R = n_rows > 32 ? 64 : 32; W = 8; }
+    else if (n_rows > 32 && blocks <= 2) { kern = scores_kernel<4, 2, 256>; R = 64; W = 4; }
+    else if (n_rows > 32 && blocks <= 4) { kern = scores_kernel<4, 4, 512>; R = 64; W = 8; }
+    else if (n_rows > 16 && blocks <= 4) { kern = scores_kernel<2, 4, 256>; R = 32; W = 4; }
     else if (n_rows > 16 && blocks <= 8) { kern = scores_kernel<2, 8, 512>; R = 32; W = 8; }
     else if (blocks <= 4) { kern = scores_kernel<1, 4, 256>; R = 16; W = 4; }
     else if (blocks <= 8) { kern = scores_kernel<1, 8, 512>; R = 16; W = 8; }
     else { kern = scores_kernel<1, 18, 768>; R = 16; W = 12; }
     p.tiles = (int)((n_rows + R - 1) / R);
+    const int64_t tokens = R / b.group + 2 < b.max_q ? R / b.group + 2 : b.max_q;    // that a tile of rows may touch
+    p.far_rows = tokens * b.n_heads * b.ld * 8 >= 0x7fffffffll;
     // Enough workgroups to fill the chip several times over (sequences differ in length), each with a tile of keys per
     // wavefront at least.
-    const int64_t units = (int64_t)b.n_seq * b.n_kv_heads * p.tiles, wanted = (W == 4 ? 32ll : 2ll) * ctx->num_cu;
+    const int64_t units = pairs * p.tiles, wanted = (blocks <= 4 && R == 16 ? 32ll : 2ll) * ctx->num_cu;
     int64_t chunks = (wanted + units - 1) / units;
     const int64_t most = (b.kv_cap + 16 * W - 1) / (16 * W);
-    if (chunks > most) chunks = most;
+    if (chunks > most || many) chunks = most;
     if (chunks < 1) chunks = 1;
     p.chunk = (int)(((b.kv_cap + chunks - 1) / chunks + 16 * W - 1) / (16 * W) * (16 * W));
     p.chunks = (b.kv_cap + p.chunk - 1) / p.chunk;
-    const int64_t grid = Unit::grid(b, p.tiles, p.chunks);
+    p.parts = Unit::parts(b, p.chunks);
+    const int64_t grid = Unit::grid(b, p.tiles, p.chunks, p.parts);
     if (grid > 0x7fffffffll) return comet_fail(ctx, COMET_ECAP, "%s: too many rows", what);
     hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(64 * W), 0, ctx->stream, p);
     COMET_LAUNCH_CHECK(ctx, what);

@@ -10,12 +10,15 @@
 #include "digits.h"
 #include "kv_batch.h"
 
+#include <type_traits>
+
 namespace comet_attn {
 
 using comet_gemm::digits_to_planes;
 using comet_gemm::to_digits;
 
 typedef int v4i __attribute__((ext_vector_type(4)));
+typedef u32 v2u __attribute__((ext_vector_type(2)));
 typedef u64 u64x2 __attribute__((ext_vector_type(2)));
 
 struct ProductParams {
@@ -32,6 +35,8 @@ struct ProductParams {
     int tiles;           // row tiles of one key head (host bound)
     int groups;          // column groups of the values
     int chunks, chunk;   // pieces the keys are cut into, keys of a piece
+    int parts;           // XCDs that share the units of a piece
+    bool far_rows;       // scores: the rows of a tile may be 2 GB apart or more
 };
 
 // Sixteen words of a lane in slot order -> its unit of every digit.
@@ -63,21 +68,28 @@ __device__ __forceinline__ u64 word_of(const v4i (&acc)[8], int e) {
 }
 
 // The work of a workgroup: a piece of the keys (chunk) of a (sequence, key head), and which of the `inner` units that read
-// the same cached rows it is.  Those follow each other on one of the eight XCDs, to which workgroups are dealt in turn.
+// the same cached rows it is.  Those follow each other on one of the eight XCDs, to which workgroups are dealt in turn; where
+// there are few pieces, a piece's units are dealt to several XCDs (parts), so that all have the same number.
 struct Unit {
     int s, kvh, chunk, inner;
     bool live;
-    __device__ __forceinline__ Unit(const Batch& b, int n_inner, int chunks) {
-        const unsigned q = blockIdx.x >> 3, group = (q / (unsigned)n_inner) * 8 + (blockIdx.x & 7);
-        const unsigned pair = group / (unsigned)chunks;
-        inner = (int)(q % (unsigned)n_inner);
-        chunk = (int)(group % (unsigned)chunks);
-        live = pair < (unsigned)(b.n_seq * b.n_kv_heads);
+    __device__ __forceinline__ Unit(const Batch& b, int n_inner, int chunks, int parts) {
+        const unsigned per = ((unsigned)n_inner + parts - 1) / (unsigned)parts;
+        const unsigned q = blockIdx.x >> 3, group = (q / per) * 8 + (blockIdx.x & 7);
+        const unsigned piece = group / (unsigned)parts, pair = piece / (unsigned)chunks;
+        inner = (int)(q % per * (unsigned)parts + group % (unsigned)parts);
+        chunk = (int)(piece % (unsigned)chunks);
+        live = pair < (unsigned)(b.n_seq * b.n_kv_heads) && inner < n_inner;
         s = (int)(pair / (unsigned)b.n_kv_heads);
         kvh = (int)(pair % (unsigned)b.n_kv_heads);
     }
-    static int64_t grid(const Batch& b, int64_t n_inner, int64_t chunks) {
-        return ((int64_t)b.n_seq * b.n_kv_heads * chunks + 7) / 8 * 8 * n_inner;
+    static int parts(const Batch& b, int64_t chunks) {
+        const int64_t pieces = (int64_t)b.n_seq * b.n_kv_heads * chunks;
+        if (pieces >= 64) return 1;
+        return pieces % 8 == 0 ? 1 : pieces % 4 == 0 ? 2 : pieces % 2 == 0 ? 4 : 8;
+    }
+    static int64_t grid(const Batch& b, int64_t n_inner, int64_t chunks, int parts) {
+        return ((int64_t)b.n_seq * b.n_kv_heads * chunks * parts + 7) / 8 * 8 * ((n_inner + parts - 1) / parts);
     }
 };
 
@@ -85,8 +97,11 @@ struct Unit {
 // kvh * group + r % group of token r / group.
 template <int R>
 struct RowTile {
-    int row[R], sees[R];
+    __align__(16) int row[R];      // -1 beyond the last
+    __align__(16) int sees[R];
+    int row0;                      // the first row (a uniform value, the smallest there is)
     __device__ __forceinline__ void fill(const Batch& b, const Sequence& sq, int kvh, int r0) {
+        if (threadIdx.x == 0) row0 = (sq.q0 + r0 / b.group) * b.n_heads + kvh * b.group;
         const int r = r0 + (int)threadIdx.x;
         if ((int)threadIdx.x < R) {
             const int n = (sq.nq < b.max_q ? sq.nq : b.max_q) * b.group;
@@ -115,8 +130,8 @@ struct RowTile {
 template <int RF>
 __device__ __forceinline__ void multiply_block(v4i (&acc)[RF][8], const v4i (&f)[8], const unsigned char* at) {
     constexpr int N = 8 * RF, DEPTH = RF == 1 ? 2 : 4, R = 16 * RF;
-    auto digit = [](int n) { const int q = n / (2 * RF); return n & 1 ? 7 - q : q; };
-    auto sub = [](int n) { return n % (2 * RF) / 2; };
+    auto digit = [](int n) { const int q = n / (2 * RF); return n / RF & 1 ? 7 - q : q; };
+    auto sub = [](int n) { return n % RF; };
     auto read = [&](int n) { return *reinterpret_cast<const v4i*>(at + (digit(n) * 4 * R + sub(n) * 16) * 16); };
     v4i a[DEPTH];
 #pragma unroll
@@ -129,6 +144,108 @@ __device__ __forceinline__ void multiply_block(v4i (&acc)[RF][8], const v4i (&f)
             if (t + u < 8) acc[i][t + u] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[n % DEPTH], f[u], acc[i][t + u], 0, 0, 0);
         if (n + DEPTH < N) a[n % DEPTH] = read(n + DEPTH);
         __builtin_amdgcn_sched_barrier(0);
+    }
+}
+
+// LDS accesses done, then meet the other wavefronts (loads from memory stay in flight).
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// Words 2 J .. 2 J + 2 N - 1 of the sixteen of the lane's row in a block of 64 that begins at key0 (ld is even: rows are 16-byte
+// aligned), and what does not count of them made zero.  The second step uses the words, so it stays away from the loads.
+template <int J, int N>
+__device__ __forceinline__ void load_row(const u64* row, int key0, int ld, int g, u64x2 (&w)[N]) {
+    if (key0 + 64 <= ld) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) w[j] = *reinterpret_cast<const u64x2*>(row + key0 + 8 * (J + j) + 2 * g);
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const int key = key0 + 8 * (J + j) + 2 * g;
+            w[j] = *reinterpret_cast<const u64x2*>(row + (key < ld ? key : ld - 2));
+        }
+    }
+}
+template <int J, int N>
+__device__ __forceinline__ void clear_beyond(u64x2 (&w)[N], int key0, int n, int g) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const int key = key0 + 8 * (J + j) + 2 * g;
+        w[j].x = key < n ? w[j].x : 0;
+        w[j].y = key + 1 < n ? w[j].y : 0;
+    }
+}
+
+// The blocks of a workgroup of eight wavefronts that multiplies 16 RF rows with sixteen columns of each, block by block: the rows'
+// digits of both halves of the stacked contraction ([E | A]) go through one of two LDS stages while the other is
+// multiplied; a wavefront's column words go straight into its registers, half a block ahead.
+//   * WORKS: the wavefront has columns;  FEEDS: it has rows to convert, of the half and at the place that `put_at` says.
+//   * The two wavefronts of a SIMD are out of step: one converts its column behind the barrier, the other (LATE) ahead of it,
+//     so that one multiplies while the other converts.
+//   * HALVES = 2: a wavefront multiplies both halves, and half a unit of every digit of the rows is on its way at a time, so
+//     that the words fit the registers beside the rest.  HALVES = 1: it multiplies half h0 only.
+// Source: row<J>(block, w) and clear<J>(block, w), words 2 J .. of the lane's row (load_row); column(half, block, w).
+// Blocks are taken from `start` on, around the end.
+template <int RF, int HALVES, bool WORKS, bool FEEDS, bool LATE, class Source>
+__device__ __forceinline__ void sweep_blocks(v4i (&acc)[RF][8], const Source& src, int blocks, int start, int h0,
+                                             unsigned char* put_at, const unsigned char* get_at) {
+    constexpr int R = 16 * RF, HALF = R * 512, STAGE = 2 * HALF, WORDS = HALVES == 2 ? 4 : 8;
+    u64x2 w[WORDS], v[8];
+    v4i f[8];
+    auto request = [&]<int J>(std::integral_constant<int, J>, int blk) {
+        if constexpr (FEEDS) src.template row<J>(blk, w);
+    };
+    auto feed = [&]<int J>(std::integral_constant<int, J>, int blk, int st) {
+        if constexpr (FEEDS) {
+            src.template clear<J>(blk, w);
+#pragma unroll
+            for (int o = 0; o < WORDS / 4; ++o) {
+                u64 x[8], plane[8];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) { x[2 * i] = to_digits(w[4 * o + i].x); x[2 * i + 1] = to_digits(w[4 * o + i].y); }
+                digits_to_planes(x, plane);
+#pragma unroll
+                for (int t = 0; t < 8; ++t)
+                    *reinterpret_cast<u64*>(put_at + st * STAGE + t * 4 * R * 16 + 8 * (J / 4 + o)) = plane[t];
+            }
+        }
+    };
+    const std::integral_constant<int, 0> lower{};
+    const std::integral_constant<int, 4> upper{};
+    int blk = start;
+    request(lower, blk);
+    if constexpr (WORKS) src.column(h0, blk, v);
+    feed(lower, blk, 0);
+    if constexpr (HALVES == 2) {
+        request(upper, blk);
+        feed(upper, blk, 0);
+    }
+    if constexpr (WORKS && LATE) to_units(v, f);
+    for (int n = 0; n < blocks; ++n) {
+        lds_barrier();
+        const int next = blk + 1 < blocks ? blk + 1 : 0, st = (n + 1) & 1;
+        const unsigned char* const from = get_at + (n & 1) * STAGE;
+        if constexpr (WORKS) {
+            if constexpr (!LATE) to_units(v, f);
+            __builtin_amdgcn_sched_barrier(0);
+            src.column(HALVES == 2 ? 1 : h0, HALVES == 2 ? blk : next, v);
+        }
+        request(lower, next);
+        if constexpr (WORKS) multiply_block<RF>(acc, f, HALVES == 2 ? from : from + h0 * HALF);
+        if constexpr (HALVES == 2) {
+            if constexpr (WORKS) {
+                to_units(v, f);
+                __builtin_amdgcn_sched_barrier(0);
+                src.column(0, next, v);
+            }
+            feed(lower, next, st);
+            request(upper, next);
+            if constexpr (WORKS) multiply_block<RF>(acc, f, from + HALF);
+            feed(upper, next, st);
+        } else {
+            feed(lower, next, st);
+        }
+        if constexpr (WORKS && LATE) to_units(v, f);
+        blk = next;
     }
 }
 

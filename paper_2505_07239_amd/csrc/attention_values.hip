@@ -14,7 +14,6 @@
 // values_finish_kernel adds up.
 #include "attention_tile.h"
 
-#include <type_traits>
 
 using namespace comet_attn;
 
@@ -50,34 +49,6 @@ __device__ __forceinline__ void load_column(const u64* pool, const int* slots, u
     }
 }
 
-// LDS accesses done, then meet the other wavefronts (loads from memory stay in flight).
-__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
-
-// Words 2 J .. 2 J + 2 N - 1 of the sixteen of the lane's row in a block of keys (ld is even: rows are 16-byte aligned), and
-// what does not count of them made zero.  The second step uses the words, so it stays away from the loads.
-template <int J, int N>
-__device__ __forceinline__ void load_row(const u64* row, int key0, int ld, int g, u64x2 (&w)[N]) {
-    if (key0 + 64 <= ld) {
-#pragma unroll
-        for (int j = 0; j < N; ++j) w[j] = *reinterpret_cast<const u64x2*>(row + key0 + 8 * (J + j) + 2 * g);
-    } else {
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-            const int key = key0 + 8 * (J + j) + 2 * g;
-            w[j] = *reinterpret_cast<const u64x2*>(row + (key < ld ? key : ld - 2));
-        }
-    }
-}
-template <int J, int N>
-__device__ __forceinline__ void clear_unseen(u64x2 (&w)[N], int key0, int sees, int g) {
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-        const int key = key0 + 8 * (J + j) + 2 * g;
-        w[j].x = key < sees ? w[j].x : 0;
-        w[j].y = key + 1 < sees ? w[j].y : 0;
-    }
-}
-
 __device__ __forceinline__ void write_word(const ProductParams& p, int row, int col, u64 sum) {
     const size_t at = (size_t)row * p.d + col;
     u64 z = rescale(p.party, p.C[at] + sum, p.frac);
@@ -97,7 +68,7 @@ __global__ __launch_bounds__(NT) void values_few_kernel(ProductParams p) {
     __shared__ RowTile<R> tile;
     __shared__ u64 sums[R * COLS];
     const Batch& b = p.b;
-    const Unit unit(b, p.tiles * p.groups, p.chunks);
+    const Unit unit(b, p.tiles * p.groups, p.chunks, p.parts);
     if (!unit.live) return;
     const int rt = p.tiles - 1 - unit.inner / p.groups;       // (the rows that see most come first)
     const int cg = unit.inner % p.groups;
@@ -138,7 +109,7 @@ __global__ __launch_bounds__(NT) void values_few_kernel(ProductParams p) {
             u64x2 w[8];
             v4i x[8];
             load_row<0>(h ? a : e, key0, b.ld, g, w);
-            if (key0 + 64 > least) clear_unseen<0>(w, key0, sees, g);
+            if (key0 + 64 > least) clear_beyond<0>(w, key0, sees, g);
             to_units(w, x);
 #pragma unroll
             for (int c = 0; c < CT; ++c) {
@@ -164,6 +135,23 @@ __global__ __launch_bounds__(NT) void values_few_kernel(ProductParams p) {
     }
 }
 
+// What a wavefront of values_many_kernel reads: its row of weights, its column of the cached rows.
+struct Source {
+    const u64 *weights, *X, *F;
+    const int* slots;
+    int first, ld, sees, least, g;
+    u32 row_bytes, lane_at;
+    template <int J, int N>
+    __device__ __forceinline__ void row(int blk, u64x2 (&w)[N]) const { load_row<J>(weights, first + 64 * blk, ld, g, w); }
+    template <int J, int N>
+    __device__ __forceinline__ void clear(int blk, u64x2 (&w)[N]) const {
+        if (first + 64 * blk + 64 > least) clear_beyond<J>(w, first + 64 * blk, sees, g);
+    }
+    __device__ __forceinline__ void column(int h, int blk, u64x2 (&v)[8]) const {
+        load_column(h ? F : X, slots + 4 * blk, row_bytes, lane_at, v);
+    }
+};
+
 // COLW: wavefronts side by side along the columns; 4: the two halves of the workgroup take E X and A F.
 template <int RF, int COLW>
 __global__ __launch_bounds__(NT) void values_many_kernel(ProductParams p) {
@@ -172,7 +160,7 @@ __global__ __launch_bounds__(NT) void values_many_kernel(ProductParams p) {
     __shared__ __align__(16) int slots[GROUPS16];
     __shared__ RowTile<R> tile;
     const Batch& b = p.b;
-    const Unit unit(b, p.tiles * p.groups, p.chunks);
+    const Unit unit(b, p.tiles * p.groups, p.chunks, p.parts);
     if (!unit.live) return;
     const int rt = p.tiles - 1 - unit.inner / p.groups;       // (the rows that see most come first)
     const int cg = unit.inner % p.groups;
@@ -211,80 +199,13 @@ __global__ __launch_bounds__(NT) void values_many_kernel(ProductParams p) {
 #pragma unroll
         for (int s = 0; s < 8; ++s) acc[i][s] = v4i{0, 0, 0, 0};
     const int blocks = end > first ? (end - first + 63) / 64 : 0;
-    // The two wavefronts of a SIMD are out of step: one converts its column behind the barrier, the other ahead of it, so
-    // that one multiplies while the other converts.
+    // Every second row tile begins in the middle: rows of weights are a few pages of memory apart, and workgroups that all read
+    // the same columns of them meet in the same few channels (512 rows of 4608 words: 784 us, and 559 with two
+    // beginnings; four and eight are no better, and cost hits in L2).
+    const int start = rt & 1 ? blocks / 2 : 0;
+    const Source src = {weights, p.X, p.F, slots, first, b.ld, csees, least, g, row_bytes, lane_at};
     auto sweep = [&]<bool WORKS, bool FEEDS, bool LATE>() {
-        // (with eight column tiles half a unit of every digit at a time: the words on their way then fit beside the rest)
-        constexpr int WORDS = COLW == 8 ? 4 : 8;
-        u64x2 w[WORDS], v[8];
-        v4i f[8];
-        auto request = [&]<int H>(std::integral_constant<int, H>, int key0) {
-            if constexpr (FEEDS) load_row<4 * H>(weights, key0, b.ld, g, w);
-        };
-        auto feed = [&]<int H>(std::integral_constant<int, H>, int key0, int st) {
-            if constexpr (FEEDS) {
-                if (key0 + 64 > least) clear_unseen<4 * H>(w, key0, csees, g);
-#pragma unroll
-                for (int o = 0; o < WORDS / 4; ++o) {
-                    u64 x[8], plane[8];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) { x[2 * i] = to_digits(w[4 * o + i].x); x[2 * i + 1] = to_digits(w[4 * o + i].y); }
-                    digits_to_planes(x, plane);
-#pragma unroll
-                    for (int t = 0; t < 8; ++t)
-                        *reinterpret_cast<u64*>(put_at + st * STAGE + t * 4 * R * 16 + 8 * (H + o)) = plane[t];
-                }
-            }
-        };
-        const std::integral_constant<int, 0> lower{};
-        const std::integral_constant<int, 1> upper{};
-        // Every second row tile begins in the middle: rows of weights are a few pages of memory apart, and workgroups that all
-        // read the same columns of them meet in the same few channels (512 rows of 4608 words: 784 us, and 600 with two
-        // beginnings; four and eight are no better, and cost hits in L2).
-        int blk = rt & 1 ? blocks / 2 : 0, key0 = first + 64 * blk;
-        request(lower, key0);
-        if constexpr (WORKS) load_column(h0 ? p.F : p.X, slots + 4 * blk, row_bytes, lane_at, v);
-        feed(lower, key0, 0);
-        if constexpr (COLW == 8) {
-            request(upper, key0);
-            feed(upper, key0, 0);
-        }
-        if constexpr (WORKS && LATE) to_units(v, f);
-        for (int n = 0; n < blocks; ++n) {
-            lds_barrier();
-            const int next = blk + 1 < blocks ? blk + 1 : 0, st = (n + 1) & 1;
-            key0 = first + 64 * next;
-            const unsigned char* const from = get_at + (n & 1) * STAGE;
-            if constexpr (COLW == 8) {
-                if constexpr (WORKS) {
-                    if constexpr (!LATE) to_units(v, f);
-                    __builtin_amdgcn_sched_barrier(0);
-                    load_column(p.F, slots + 4 * blk, row_bytes, lane_at, v);
-                }
-                request(lower, key0);
-                if constexpr (WORKS) {
-                    multiply_block<RF>(acc, f, from);
-                    to_units(v, f);
-                    __builtin_amdgcn_sched_barrier(0);
-                    load_column(p.X, slots + 4 * next, row_bytes, lane_at, v);
-                }
-                feed(lower, key0, st);
-                request(upper, key0);
-                if constexpr (WORKS) multiply_block<RF>(acc, f, from + HALF);
-                feed(upper, key0, st);
-            } else {
-                if constexpr (WORKS) {
-                    if constexpr (!LATE) to_units(v, f);
-                    __builtin_amdgcn_sched_barrier(0);
-                    load_column(h0 ? p.F : p.X, slots + 4 * next, row_bytes, lane_at, v);
-                }
-                request(lower, key0);
-                if constexpr (WORKS) multiply_block<RF>(acc, f, from + h0 * HALF);
-                feed(lower, key0, st);
-            }
-            if constexpr (WORKS && LATE) to_units(v, f);
-            blk = next;
-        }
+        sweep_blocks<RF, COLW == 8 ? 2 : 1, WORKS, FEEDS, LATE>(acc, src, blocks, start, h0, put_at, get_at);
     };
     if (blocks > 0) {
         if (wave < 4) {                                       // (these feed, whatever RF is)
@@ -298,9 +219,9 @@ __global__ __launch_bounds__(NT) void values_many_kernel(ProductParams p) {
             else sweep.template operator()<false, false, true>();
         }
     }
-    if (COLW == 4) {
+    u64* const sums = reinterpret_cast<u64*>(stage);
+    if constexpr (COLW == 4) {
         // the halves of the workgroup meet in LDS
-        u64* const sums = reinterpret_cast<u64*>(stage);
         __syncthreads();
         if (h0 == 1 && works)
 #pragma unroll
@@ -308,23 +229,32 @@ __global__ __launch_bounds__(NT) void values_many_kernel(ProductParams p) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) sums[(16 * i + 4 * g + e) * COLS + cw * 16 + r] = word_of(acc[i], e);
         __syncthreads();
-        if (h0 == 0 && works && col < p.d)
-#pragma unroll
-            for (int i = 0; i < RF; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int rr = 16 * i + 4 * g + e;
-                    if (tile.row[rr] >= 0) put(p, unit.chunk, tile.row[rr], col, word_of(acc[i], e) + sums[rr * COLS + cw * 16 + r]);
-                }
-    } else if (works && col < p.d) {
+        if (h0 == 1) return;
+    }
+    if (!works || col >= p.d) return;
+    // all loads first: Z may be C or M, so the compiler would wait for every store before the next load
+    u64 c[RF][4], m[RF][4];
+    if (!p.part)
 #pragma unroll
         for (int i = 0; i < RF; ++i)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const int rr = 16 * i + 4 * g + e;
-                if (tile.row[rr] >= 0) put(p, unit.chunk, tile.row[rr], col, word_of(acc[i], e));
+                const int row = tile.row[16 * i + 4 * g + e];
+                const size_t at = (size_t)(row < 0 ? 0 : row) * p.d + col;
+                c[i][e] = p.C[at];
+                m[i][e] = p.M ? p.M[at] : 0;
             }
-    }
+#pragma unroll
+    for (int i = 0; i < RF; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int rr = 16 * i + 4 * g + e, row = tile.row[rr];
+            u64 z = word_of(acc[i], e);
+            if constexpr (COLW == 4) z += sums[rr * COLS + cw * 16 + r];
+            if (row < 0) continue;
+            if (p.part) p.part[((size_t)unit.chunk * b.n_tok * b.n_heads + row) * p.d + col] = z;
+            else p.Z[(size_t)row * p.d + col] = rescale(p.party, c[i][e] + z, p.frac) - m[i][e];
+        }
 }
 
 // Adds up the pieces of a row that have been written: those that begin before the last key it sees, and the first.
@@ -393,7 +323,8 @@ int comet_attn::launch_values(comet_ctx* ctx, const char* what, ProductParams& p
     if (p.chunk < 64) p.chunk = 64;
     p.chunks = b.kv_cap > 0 ? (b.kv_cap + p.chunk - 1) / p.chunk : 1;
     p.part = p.chunks > 1 ? (u64*)ws : nullptr;
-    const int64_t grid = Unit::grid(b, (int64_t)p.tiles * p.groups, p.chunks);
+    p.parts = Unit::parts(b, p.chunks);
+    const int64_t grid = Unit::grid(b, (int64_t)p.tiles * p.groups, p.chunks, p.parts);
     const int pieces = (p.d + 255) / 256;
     const int64_t finish = (int64_t)b.n_seq * b.max_q * b.n_heads * pieces;
     if (grid > 0x7fffffffll || finish > 0x7fffffffll) return comet_fail(ctx, COMET_ECAP, "%s: too many rows", what);
