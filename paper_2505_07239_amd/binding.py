@@ -135,6 +135,7 @@ class _NoHost:
         return None
 
     elementwise = gather = open_planes = compact = share = group = _decline
+    cache_write = cache_read = rotate = product = weights = _decline
 
 
 _Host = None                       # set by load_library()
@@ -248,7 +249,7 @@ class KVBatch:
         self.n_tok, self.n_heads, self.n_kv_heads, self.page_size = n_tok, n_heads, n_kv_heads, page_size
         self.struct = _Batch(n_seq, n_tok, n_heads, n_kv_heads, page_size, block_table.shape[1], max_q,
                              CAUSAL if causal else 0, *[_ptr(t) for t in (q_start, kv_len, block_table, head_mask)])
-        self.ref = ctypes.byref(self.struct)
+        self.ref, self.address = ctypes.byref(self.struct), ctypes.addressof(self.struct)
 
 
 def _ints(t: torch.Tensor, what: str) -> torch.Tensor:
@@ -689,6 +690,10 @@ class Context:
         """F[slots] = d_0 + d_1 and X_i[slots] = b_i + party * F, in place.  ``d_0``, ``d_1``, ``b_i``: [n_tok, ...]
         with the words of a slot; ``slots`` int32 [n_tok], -1 for padding; pools of any shape whose elements are n_slots
         times the words of a slot."""
+        r = self._host.cache_write(party, d_0, d_1, b_i, slots, f_pool, x_pool)
+        if r is not None:
+            self._made(r)
+            return
         _words(d_0, "d_0"), _words(d_1, "d_1"), _words(b_i, "b_i"), _words(f_pool, "f_pool"), _words(x_pool, "x_pool")
         n_tok, width, n_slots = self._rows(slots, d_0, f_pool, x_pool)
         if d_1.shape != d_0.shape or b_i.shape != d_0.shape:
@@ -701,6 +706,11 @@ class Context:
     def cache_read(self, party, f_pool, x_pool, slots, width=None, out=None):
         """(F[slots], X_i[slots] - party * F[slots]): cached rows as E and A_i of a share product, [n_tok, width].
         ``width``: words of a slot (default: those of ``out``, or the pools' elements per entry of their first axis)."""
+        if out is not None and width is None and len(out) == 2:
+            r = self._host.cache_read(party, f_pool, x_pool, slots, out[0], out[1])
+            if r is not None:
+                self._made(r)
+                return out[0], out[1]
         _words(f_pool, "f_pool"), _words(x_pool, "x_pool"), _ints(slots, "slots")
         if out is None:
             width = f_pool[0].numel() if width is None else width
@@ -733,6 +743,10 @@ class Context:
                      out=None):
         """Rescaling, position rotation and masking of queries or keys: ``x_i`` [n_tok, n_heads * head_dim], possibly a column
         range of a wider matrix; ``cos``, ``sin`` [n_pos, rot_dim / 2] fixed-point words; ``positions`` int32 [n_tok]."""
+        if out is not None:
+            r = self._host.rotate(party, x_i, positions, cos, sin, n_heads, shift, frac_bits, m_i, interleaved, out)
+            if r is not None:
+                return self._made(r)
         if x_i.dtype != torch.int64 or not x_i.is_cuda or x_i.dim() != 2 or (x_i.shape[1] > 1 and x_i.stride(1) != 1):
             raise TypeError("x_i must be a 2-D int64 tensor on the GPU with contiguous rows")
         _words(cos, "cos"), _words(sin, "sin"), _ints(positions, "positions")
@@ -754,6 +768,10 @@ class Context:
         return out
 
     def _product(self, call, op, party, batch, e, a_i, f_pool, x_pool, c_i, frac_bits, m_i, out):
+        if out is not None and batch.device == self.device:
+            r = self._host.product(op == OP_SCORES, party, batch.address, e, a_i, f_pool, x_pool, c_i, frac_bits, m_i, out)
+            if r is not None:
+                return self._made(r)
         for t, what in ((e, "E"), (a_i, "A_i"), (f_pool, "f_pool"), (x_pool, "x_pool"), (c_i, "C_i")):
             _words(t, what)
         if e.dim() != 3 or c_i.dim() != 3 or f_pool.dim() != 4:
@@ -793,6 +811,12 @@ class Context:
     def attention_weights(self, party, batch, d_0, d_1, r_i, r2_i, bias, frac_bits=16, m_i=None, out=None):
         """(shares of w = (s + bias)^2 - m, shares of the row sums of w) from masked scores d_0 + d_1 = s - r (``d_1``
         None: ``d_0`` is already opened) and a square pair (r, r^2); all [n_tok, n_heads, ld].  ``out``: (weights, sums)."""
+        bias &= 2 ** 64 - 1
+        if out is not None and len(out) == 2 and batch.device == self.device:
+            r = self._host.weights(party, batch.address, d_0, d_1, r_i, r2_i, bias, frac_bits, m_i, out[0], out[1])
+            if r is not None:
+                self._made(r)
+                return out[0], out[1]
         for t, what in ((d_0, "d_0"), (r_i, "r_i"), (r2_i, "r2_i")):
             _words(t, what)
         if d_0.dim() != 3:
@@ -807,7 +831,7 @@ class Context:
         _shape(_words(w, "out"), shape, "out"), _shape(_words(sums, "sums"), shape[:2], "sums")
         self._here(d_0, d_1, r_i, r2_i, m_i, w, sums, batch.tensors[0])
         self._sync_stream()
-        self._check(self.lib.comet_attention_weights(self.h, party, batch.ref, shape[2], frac_bits, bias & (2 ** 64 - 1),
+        self._check(self.lib.comet_attention_weights(self.h, party, batch.ref, shape[2], frac_bits, bias,
                                                      _ptr(d_0), _ptr(d_1), _ptr(r_i), _ptr(r2_i), _ptr(m_i), _ptr(w),
                                                      _ptr(sums)))
         return w, sums

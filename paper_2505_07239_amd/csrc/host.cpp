@@ -38,6 +38,12 @@ struct Library {
     decltype(&comet_somm_share_unopened) somm_share_unopened;
     decltype(&comet_simm_share_unopened) simm_share_unopened;
     decltype(&comet_share_group) share_group;
+    decltype(&comet_cache_write) cache_write;
+    decltype(&comet_cache_read) cache_read;
+    decltype(&comet_rotate_share) rotate_share;
+    decltype(&comet_attention_scores) attention_scores;
+    decltype(&comet_attention_weights) attention_weights;
+    decltype(&comet_attention_values) attention_values;
 } lib;
 bool bound = false;
 PyTypeObject* planes_type = nullptr;      // binding.WeightPlanes
@@ -388,6 +394,160 @@ PyObject* group(Host* self, PyObject* const* arg, Py_ssize_t nargs) {
 // ---------------------------------------------------------------------------
 // the type and the module
 // ---------------------------------------------------------------------------
+// ---- attention over a cache of shares: results are the caller's, everything is on the context's device ----
+
+const Tensor* here(Host* self, const Tensor* t) { return t && t->get_device() == self->device ? t : nullptr; }
+const Tensor* words_here(Host* self, PyObject* o) { return here(self, words(o)); }
+
+// words, or None (*t null); false to decline
+bool maybe_words(Host* self, PyObject* o, const Tensor** t) {
+    *t = o == Py_None ? nullptr : words_here(self, o);
+    return *t || o == Py_None;
+}
+bool same(const Tensor* a, const Tensor* b) { return a->sizes().equals(b->sizes()); }
+bool cube(const Tensor* t, int64_t a, int64_t b) { return t->dim() == 3 && t->size(0) == a && t->size(1) == b; }
+uint64_t* data(const Tensor* t) { return t ? u64(*t) : nullptr; }
+
+// A batch comes as the address of its struct (KVBatch keeps it, and its device is the context's: binding.py).
+const comet_kv_batch* batch_at(PyObject* o) {
+    const comet_kv_batch* b = PyLong_CheckExact(o) ? static_cast<const comet_kv_batch*>(PyLong_AsVoidPtr(o)) : nullptr;
+    PyErr_Clear();
+    return b;
+}
+
+// tokens, words of a slot and slots of a cache call; false to decline
+bool cache_rows(Host* self, const Tensor* slots, const Tensor* rows, const Tensor* f, const Tensor* x, int64_t* n_tok,
+                int64_t* width, int64_t* n_slots) {
+    if (!here(self, slots) || !rows || !f || !x || slots->dim() != 1 || rows->dim() < 2 || rows->size(0) != slots->size(0)) return false;
+    *n_tok = slots->size(0);
+    *width = *n_tok > 0 ? rows->numel() / *n_tok : 0;
+    if (*width == 0 || f->numel() != x->numel() || f->numel() % *width != 0) return false;
+    *n_slots = f->numel() / *width;
+    return true;
+}
+
+// (party, d_0, d_1, b, slots, f_pool, x_pool) -> True
+PyObject* cache_write(Host* self, PyObject* const* arg, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    READY(7);
+    long long party;
+    const Tensor *d0 = words_here(self, arg[1]), *d1 = words_here(self, arg[2]), *b = words_here(self, arg[3]);
+    const Tensor *slots = typed(arg[4], c10::kInt), *f = words_here(self, arg[5]), *x = words_here(self, arg[6]);
+    int64_t n_tok, width, n_slots;
+    if (!integer(arg[0], 0, 1, &party) || !d1 || !b || !cache_rows(self, slots, d0, f, x, &n_tok, &width, &n_slots) || !same(d0, d1) ||
+        !same(d0, b))
+        DECLINE;
+    const uint64_t *p0 = u64(*d0), *p1 = u64(*d1), *pb = u64(*b);
+    auto* ps = static_cast<const int32_t*>(slots->data_ptr());
+    uint64_t *pf = u64(*f), *px = u64(*x);
+    return call(self, THPObjectPtr::dup(Py_True),
+                [&] { return lib.cache_write(self->ctx, (int)party, p0, p1, pb, ps, n_tok, width, pf, px, n_slots); });
+    END_HANDLE_TH_ERRORS
+}
+
+// (party, f_pool, x_pool, slots, e, a) -> True
+PyObject* cache_read(Host* self, PyObject* const* arg, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    READY(6);
+    long long party;
+    const Tensor *f = words_here(self, arg[1]), *x = words_here(self, arg[2]), *slots = typed(arg[3], c10::kInt);
+    const Tensor *e = words_here(self, arg[4]), *a = words_here(self, arg[5]);
+    int64_t n_tok, width, n_slots;
+    if (!integer(arg[0], 0, 1, &party) || !a || !cache_rows(self, slots, e, f, x, &n_tok, &width, &n_slots) || !same(e, a)) DECLINE;
+    const uint64_t *pf = u64(*f), *px = u64(*x);
+    auto* ps = static_cast<const int32_t*>(slots->data_ptr());
+    uint64_t *pe = u64(*e), *pa = u64(*a);
+    return call(self, THPObjectPtr::dup(Py_True),
+                [&] { return lib.cache_read(self->ctx, (int)party, pf, px, ps, n_tok, width, n_slots, pe, pa); });
+    END_HANDLE_TH_ERRORS
+}
+
+// (party, x, positions, cos, sin, n_heads, shift, frac_bits, m, interleaved, out) -> out
+PyObject* rotate(Host* self, PyObject* const* arg, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    READY(11);
+    long long party, heads, shift, frac;
+    bool interleaved;
+    const Tensor *x = here(self, plain(arg[1])), *pos = here(self, typed(arg[2], c10::kInt)), *m;
+    const Tensor *c = words_here(self, arg[3]), *s = words_here(self, arg[4]), *out = words_here(self, arg[10]);
+    if (!integer(arg[0], 0, 1, &party) || !integer(arg[5], 1, INT_LIMIT, &heads) || !integer(arg[6], 0, 62, &shift) ||
+        !integer(arg[7], 0, 62, &frac) || !flag(arg[9], &interleaved) || !maybe_words(self, arg[8], &m) || !x || !pos || !c || !s || !out)
+        DECLINE;
+    if (x->scalar_type() != c10::kLong || x->dim() != 2 || (x->size(1) > 1 && x->stride(1) != 1) || c->dim() != 2 || !same(c, s)) DECLINE;
+    const int64_t n_tok = x->size(0), width = x->size(1), rot = 2 * c->size(1);
+    if (n_tok == 0 || width % heads != 0 || width / heads > INT_LIMIT || rot > INT_LIMIT || pos->dim() != 1 || pos->size(0) != n_tok ||
+        !shaped(*out, n_tok, width) || (m && !shaped(*m, n_tok, width)))
+        DECLINE;
+    const int64_t ldx = n_tok > 1 ? x->stride(0) : width, n_pos = c->size(0);
+    const uint64_t *px = u64(*x), *pc = u64(*c), *ps = u64(*s), *pm = data(m);
+    auto* pp = static_cast<const int32_t*>(pos->data_ptr());
+    uint64_t* po = u64(*out);
+    return call(self, THPObjectPtr::dup(arg[10]), [&] {
+        return lib.rotate_share(self->ctx, (int)party, px, ldx, pp, pc, ps, n_pos, n_tok, (int)heads, (int)(width / heads), (int)rot,
+                                interleaved, (int)shift, (int)frac, pm, po);
+    });
+    END_HANDLE_TH_ERRORS
+}
+
+// (scores?, party, batch, e, a, f_pool, x_pool, c, frac_bits, m, out) -> out
+PyObject* product(Host* self, PyObject* const* arg, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    READY(11);
+    bool scores;
+    long long party, frac;
+    const comet_kv_batch* b = batch_at(arg[2]);
+    const Tensor *e = words_here(self, arg[3]), *a = words_here(self, arg[4]), *f = words_here(self, arg[5]), *m;
+    const Tensor *x = words_here(self, arg[6]), *c = words_here(self, arg[7]), *out = words_here(self, arg[10]);
+    if (!flag(arg[0], &scores) || !integer(arg[1], 0, 1, &party) || !integer(arg[8], 0, 62, &frac) || !maybe_words(self, arg[9], &m) ||
+        !b || !e || !a || !f || !x || !c || !out)
+        DECLINE;
+    if (!cube(e, b->n_tok, b->n_heads) || !same(e, a) || !cube(c, b->n_tok, b->n_heads) || !same(c, out) || (m && !same(c, m)) ||
+        f->dim() != 4 || f->size(1) != b->page_size || f->size(2) != b->n_kv_heads || !same(f, x))
+        DECLINE;
+    const int64_t left = e->size(2), right = c->size(2), d = scores ? left : right, ld = scores ? right : left;
+    const int64_t n_pages = f->size(0), ldp = f->size(3);
+    if (d > INT_LIMIT || ldp > INT_LIMIT) DECLINE;
+    const size_t need = lib.workspace_bytes(scores ? COMET_OP_SCORES : COMET_OP_VALUES, (int64_t)b->n_tok * b->n_heads, left, right, 0);
+    Tensor ws;
+    if (need > 0) ws = at::empty({(int64_t)need}, e->options().dtype(c10::kByte).requires_grad(false));
+    void* pw = need > 0 ? ws.data_ptr() : nullptr;
+    const uint64_t *pe = u64(*e), *pa = u64(*a), *pf = u64(*f), *px = u64(*x), *pc = u64(*c), *pm = data(m);
+    uint64_t* po = u64(*out);
+    return call(self, THPObjectPtr::dup(arg[10]), [&] {
+        return (scores ? lib.attention_scores : lib.attention_values)(self->ctx, (int)party, b, (int)d, (int)ldp, n_pages, ld, (int)frac,
+                                                                     pe, pa, pf, px, pc, pm, po, pw, need);
+    });
+    END_HANDLE_TH_ERRORS
+}
+
+// (party, batch, d_0, d_1, r, r2, bias mod 2^64, frac_bits, m, out, sums) -> True
+PyObject* weights(Host* self, PyObject* const* arg, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    READY(11);
+    long long party, frac;
+    const comet_kv_batch* b = batch_at(arg[1]);
+    const Tensor *d0 = words_here(self, arg[2]), *r = words_here(self, arg[4]), *r2 = words_here(self, arg[5]), *d1, *m;
+    const Tensor *out = words_here(self, arg[9]), *sums = words_here(self, arg[10]);
+    if (!integer(arg[0], 0, 1, &party) || !integer(arg[7], 0, 62, &frac) || !maybe_words(self, arg[3], &d1) ||
+        !maybe_words(self, arg[8], &m) || !b || !d0 || !r || !r2 || !out || !sums || !PyLong_CheckExact(arg[6]))
+        DECLINE;
+    const uint64_t bias = PyLong_AsUnsignedLongLong(arg[6]);
+    if (PyErr_Occurred()) {
+        PyErr_Clear();
+        DECLINE;
+    }
+    if (!cube(d0, b->n_tok, b->n_heads) || !same(d0, r) || !same(d0, r2) || (d1 && !same(d0, d1)) || (m && !same(d0, m)) || !same(d0, out) ||
+        !shaped(*sums, b->n_tok, b->n_heads))
+        DECLINE;
+    const int64_t ld = d0->size(2);
+    const uint64_t *p0 = u64(*d0), *p1 = data(d1), *pr = u64(*r), *pr2 = u64(*r2), *pm = data(m);
+    uint64_t *po = u64(*out), *ps = u64(*sums);
+    return call(self, THPObjectPtr::dup(Py_True), [&] {
+        return lib.attention_weights(self->ctx, (int)party, b, ld, (int)frac, bias, p0, p1, pr, pr2, pm, po, ps);
+    });
+    END_HANDLE_TH_ERRORS
+}
+
 PyObject* host_new(PyTypeObject* type, PyObject* args, PyObject*) {
     unsigned long long ctx;
     int device;
@@ -409,6 +569,7 @@ PyObject* entry(PyObject* self, PyObject* const* arg, Py_ssize_t nargs) { return
 #define ENTRY(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&entry<f>)), METH_FASTCALL, nullptr}
 
 PyMethodDef host_methods[] = {ENTRY(elementwise), ENTRY(gather), ENTRY(open_planes), ENTRY(compact), ENTRY(share), ENTRY(group),
+                              ENTRY(cache_write), ENTRY(cache_read), ENTRY(rotate), ENTRY(product), ENTRY(weights),
                               {"close", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&host_close)), METH_NOARGS, nullptr},
                               {nullptr, nullptr, 0, nullptr}};
 
@@ -435,7 +596,10 @@ PyObject* bind(PyObject*, PyObject* args) {
             find("comet_open_weight_planes_neuron_major", lib.open_weight_planes_neuron_major) &&
             find("comet_compact_mask", lib.compact_mask) && find("comet_somm_share", lib.somm_share) &&
             find("comet_simm_share", lib.simm_share) && find("comet_somm_share_unopened", lib.somm_share_unopened) &&
-            find("comet_simm_share_unopened", lib.simm_share_unopened) && find("comet_share_group", lib.share_group);
+            find("comet_simm_share_unopened", lib.simm_share_unopened) && find("comet_share_group", lib.share_group) &&
+            find("comet_cache_write", lib.cache_write) && find("comet_cache_read", lib.cache_read) &&
+            find("comet_rotate_share", lib.rotate_share) && find("comet_attention_scores", lib.attention_scores) &&
+            find("comet_attention_weights", lib.attention_weights) && find("comet_attention_values", lib.attention_values);
     if (!bound) return nullptr;
     Py_INCREF(planes);
     Py_XDECREF(planes_type);
