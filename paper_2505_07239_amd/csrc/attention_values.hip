@@ -49,21 +49,10 @@ __device__ __forceinline__ void load_column(const u64* pool, const int* slots, u
     }
 }
 
-__device__ __forceinline__ void write_word(const ProductParams& p, int row, int col, u64 sum) {
-    const size_t at = (size_t)row * p.d + col;
-    u64 z = rescale(p.party, p.C[at] + sum, p.frac);
-    if (p.M) z -= p.M[at];
-    p.Z[at] = z;
-}
-
-// Sum of a piece: the result, or a partial sum.  A piece beyond what a row tile sees is not written, but for the first.
-__device__ __forceinline__ void put(const ProductParams& p, int chunk, int row, int col, u64 sum) {
-    if (p.part) p.part[((size_t)chunk * p.b.n_tok * p.b.n_heads + row) * p.d + col] = sum;
-    else write_word(p, row, col, sum);
-}
-
+// CT: tiles of 16 columns of a wavefront.
+template <int CT>
 __global__ __launch_bounds__(NT) void values_few_kernel(ProductParams p) {
-    constexpr int R = 16, CT = 4, COLS = 16 * CT;
+    constexpr int R = 16, COLS = 16 * CT;
     __shared__ __align__(16) int slots[GROUPS16];
     __shared__ RowTile<R> tile;
     __shared__ u64 sums[R * COLS];
@@ -75,15 +64,14 @@ __global__ __launch_bounds__(NT) void values_few_kernel(ProductParams p) {
     const Sequence sq(b, unit.s);
     if (rt * R >= sq.nq * b.group) return;
     tile.fill(b, sq, unit.kvh, rt * R);
+    const int first = unit.chunk * p.chunk;
+    find_slots(slots, b, sq, first, first + p.chunk < sq.kv ? first + p.chunk : sq.kv);
+    for (int i = threadIdx.x; i < R * COLS; i += NT) sums[i] = 0;
     __syncthreads();
     int most, least;
     tile.span(most, least);
-    const int first = unit.chunk * p.chunk;
     const int end = most < first + p.chunk ? most : first + p.chunk;
     if (first >= end && unit.chunk > 0) return;
-    find_slots(slots, b, sq, first, end);
-    for (int i = threadIdx.x; i < R * COLS; i += NT) sums[i] = 0;
-    __syncthreads();
 
     const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
@@ -128,10 +116,26 @@ __global__ __launch_bounds__(NT) void values_few_kernel(ProductParams p) {
     for (int c = 0; c < CT; ++c)
 #pragma unroll
         for (int e4 = 0; e4 < 4; ++e4) atomicAdd(&sums[(4 * g + e4) * COLS + c * 16 + r], word_of(acc[c], e4));
+    // (C and M are on their way while the sums come together)
+    constexpr int EACH = (R * COLS + NT - 1) / NT;
+    u64 c[EACH], m[EACH];
+    size_t at[EACH];
+    bool live[EACH];
+#pragma unroll
+    for (int n = 0; n < EACH; ++n) {
+        const int i = n * NT + (int)threadIdx.x, col = cg * COLS + i % COLS, to = tile.row[i / COLS % R];
+        live[n] = i < R * COLS && to >= 0 && col < p.d;
+        at[n] = live[n] ? (size_t)to * p.d + col : 0;
+        c[n] = p.part ? 0 : p.C[at[n]];
+        m[n] = p.part || !p.M ? 0 : p.M[at[n]];
+    }
     __syncthreads();
-    for (int i = threadIdx.x; i < R * COLS; i += NT) {
-        const int rr = i / COLS, col = cg * COLS + i % COLS;
-        if (tile.row[rr] >= 0 && col < p.d) put(p, unit.chunk, tile.row[rr], col, sums[i]);
+#pragma unroll
+    for (int n = 0; n < EACH; ++n) {
+        if (!live[n]) continue;
+        const u64 sum = sums[n * NT + (int)threadIdx.x];
+        if (p.part) p.part[(size_t)unit.chunk * b.n_tok * b.n_heads * p.d + at[n]] = sum;
+        else p.Z[at[n]] = rescale(p.party, c[n] + sum, p.frac) - m[n];
     }
 }
 
@@ -167,14 +171,13 @@ __global__ __launch_bounds__(NT) void values_many_kernel(ProductParams p) {
     const Sequence sq(b, unit.s);
     if (rt * R >= sq.nq * b.group) return;
     tile.fill(b, sq, unit.kvh, rt * R);
+    const int first = unit.chunk * p.chunk;
+    find_slots(slots, b, sq, first, first + p.chunk < sq.kv ? first + p.chunk : sq.kv);
     __syncthreads();
     int most, least;
     tile.span(most, least);
-    const int first = unit.chunk * p.chunk;
     const int end = most < first + p.chunk ? most : first + p.chunk;
     if (first >= end && unit.chunk > 0) return;
-    find_slots(slots, b, sq, first, end);
-    __syncthreads();
 
     const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
@@ -272,7 +275,9 @@ __global__ __launch_bounds__(256) void values_finish_kernel(ProductParams p, int
     const u64* from = p.part + (size_t)row * p.d + col;
     u64 sum = from[0];
     for (int c = 1; c * p.chunk < sees; ++c) sum += from[c * all];
-    write_word(p, row, col, sum);
+    const size_t at = (size_t)row * p.d + col;
+    const u64 z = rescale(p.party, p.C[at] + sum, p.frac);
+    p.Z[at] = p.M ? z - p.M[at] : z;
 }
 
 // Pieces that the workspace of a call may hold: as many as a plane needs, and more while the partial sums of all rows
@@ -303,7 +308,13 @@ int comet_attn::launch_values(comet_ctx* ctx, const char* what, ProductParams& p
         return comet_fail(ctx, COMET_EALIGN, "%s: the workspace must be 256-byte aligned", what);
     int R, cols, step;
     void (*kern)(ProductParams);
-    if (n_rows <= 16) { kern = values_few_kernel; R = 16; cols = 64; step = 64 * W; }
+    // Up to 16 rows: four column tiles a wavefront, for whose sake the weights are loaded and split once; one where there are
+    // not workgroups for every second compute unit, and the launch is as long as a wavefront's chain of loads.
+    if (n_rows <= 16) {
+        const bool small = (int64_t)b.n_seq * b.n_kv_heads * ((p.d + 63) / 64) * ((b.kv_cap + 64 * W - 1) / (64 * W)) * 2 <= ctx->num_cu;
+        kern = small ? values_few_kernel<1> : values_few_kernel<4>;
+        R = 16; cols = small ? 16 : 64; step = 64 * W;
+    }
     else if (p.d <= 64) { kern = n_rows <= 32 ? values_many_kernel<2, 4> : values_many_kernel<4, 4>; R = n_rows <= 32 ? 32 : 64; cols = 64; step = 64; }
     else { kern = n_rows <= 32 ? values_many_kernel<2, 8> : values_many_kernel<4, 8>; R = n_rows <= 32 ? 32 : 64; cols = 128; step = 64; }
     p.tiles = (int)((n_rows + R - 1) / R);
