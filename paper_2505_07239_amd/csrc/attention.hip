@@ -85,7 +85,7 @@ int make_batch(comet_ctx* ctx, const char* what, const comet_kv_batch* in, int64
     if (in->n_seq < 0 || in->n_tok < 0 || in->n_heads < 1 || in->n_kv_heads < 1 || in->n_heads % in->n_kv_heads != 0 ||
         in->max_q < 0 || in->max_pages < 0 || in->page_size < 16 || in->page_size % 16 != 0 || (in->flags & ~COMET_CAUSAL) != 0)
         return comet_fail(ctx, COMET_EINVAL, "%s: bad batch (n_heads must be a multiple of n_kv_heads, page_size of 16)", what);
-    if (ld < 0 || (ld & 1) || n_pages < 0) return comet_fail(ctx, COMET_EINVAL, "%s: ld must be even and not negative", what);
+    if (ld < 2 || (ld & 1) || n_pages < 0) return comet_fail(ctx, COMET_EINVAL, "%s: ld must be even and at least 2", what);
     if (ld > COMET_DIM_MAX || n_pages > 0x7fffffffll || n_pages * in->page_size > 0x7fffffffll ||
         (int64_t)in->n_tok * in->n_heads > 0x7fffffffll || (int64_t)in->n_seq * in->max_q > COMET_DIM_MAX ||
         (int64_t)in->n_seq * in->n_kv_heads > COMET_DIM_MAX)

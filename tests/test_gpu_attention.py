@@ -144,6 +144,71 @@ def test_latent_rows(ctx, d, ldp, heads):
     check_values(ctx, k, d, 0, 16, True)
 
 
+@pytest.mark.parametrize("heads,kvh,new", [(40, 1, 1), (20, 1, 1), (4, 2, 1), (2, 2, 24)])
+@pytest.mark.parametrize("d,ldp", [(576, 576), (300, 320), (128, 128)])
+def test_capacity_beyond_the_lengths(ctx, heads, kvh, new, d, ldp):
+    """Calls are planned by what the operands could hold: rows of 4224 words of which a few are used, so that
+    the variants for large batches run."""
+    say("capacity heads=%d kvh=%d new=%d d=%d" % (heads, kvh, new, d))
+    k = Case(2250 + d + heads, [(new, 50 + 13 * s) for s in range(8)], heads, kvh, page=64, ldp=ldp, spare=63)
+    assert k.ld >= 4096
+    check_scores(ctx, k, d, 1, 16, True)
+    check_values(ctx, k, d, 0, 16, True)
+
+
+@pytest.mark.parametrize("new,kv,heads,kvh,d", [(70, 1500, 2, 1, 64), (40, 1300, 2, 2, 80), (3, 2100, 8, 1, 128), (20, 9000, 1, 1, 16)])
+def test_keys_in_pieces(ctx, new, kv, heads, kvh, d):
+    """Few rows over long sequences: the keys are cut into pieces, some of which begin beyond what a row sees."""
+    say("pieces new=%d kv=%d" % (new, kv))
+    k = Case(2270 + d, [(new, kv), (new, new), (1, 700)], heads, kvh, page=32, ldp=d, mask=d == 64)
+    check_scores(ctx, k, d, 0, 16, False)
+    check_values(ctx, k, d, 1, 16, True)
+
+
+def test_rows_far_apart(ctx):
+    """Rows of a tile more than 2 GB apart: 40 tokens of one head, rows of 2^23 words."""
+    say("far rows")
+    import paper_2505_07239_amd as comet
+    t, ld, d = 40, 1 << 23, 16
+    q, kv, table = ints([0, t]), ints([50]), ints(np.zeros((1, ld // 16)))
+    table[0, :4] = ints([2, 0, 1, 3])
+    batch = comet.KVBatch(t, 1, 1, q, kv, table, 16, t)
+    f, x = u64(2280, 1, 4, 16, 1, d), u64(2280, 2, 4, 16, 1, d)
+    e, a = u64(2280, 3, t, 1, d), u64(2280, 4, t, 1, d)
+    c, m = u64(2280, 5, t, 1, 64), u64(2280, 6, t, 1, 64)
+    wide = [torch.zeros(t, 1, ld, dtype=torch.int64, device="cuda") for _ in range(3)]
+    for w, v in zip(wide, (c, m, pattern(t, 1, 64))):
+        w[:, :, :64] = up(v)
+    out = ctx.attention_scores(1, batch, up(e), up(a), up(f), up(x), wide[0], 16, wide[1], out=wide[2])
+    rows = list(oa.rows([0, t], [50], 1))
+    want = oa.scores(1, rows, e, a, f, x, np.array([[2, 0, 1, 3]]), c, 16, m, pattern(t, 1, 64))
+    assert np.array_equal(down(out[:, :, :64].contiguous()), want)
+    assert not bool(out[:, :, 64:].any())
+    z = u64(2280, 7, t, 1, d)
+    got = ctx.attention_values(0, batch, out, wide[1], up(f), up(x), up(z), 16)
+    assert np.array_equal(down(got), oa.values(0, rows, want, m, f, x, np.array([[2, 0, 1, 3]]), z, 16, None, np.zeros_like(z)))
+
+
+def test_two_contexts_on_two_streams(ctx):
+    """Calls of two contexts in flight together share nothing."""
+    import paper_2505_07239_amd as comet
+    cases = [Case(2290 + i, [(1, 3000 - 500 * i), (1, 900)], 8, 2, page=64, ldp=64) for i in (0, 1)]
+    both, streams = [ctx, comet.Context(0)], [torch.cuda.Stream(), torch.cuda.Stream()]
+    ops = [[up(k.words(5, k.ld)), up(k.words(6, k.ld)), up(k.f), up(k.x), up(k.words(7, 64))] for k in cases]
+    torch.cuda.synchronize()
+    outs = [[], []]
+    for _ in range(10):
+        for i in (0, 1):
+            with torch.cuda.stream(streams[i]):
+                outs[i].append(both[i].attention_values(i, cases[i].batch, *ops[i], 16))
+    torch.cuda.synchronize()
+    for i, k in enumerate(cases):
+        want = oa.values(i, k.rows, k.words(5, k.ld), k.words(6, k.ld), k.f, k.x, k.table, k.words(7, 64), 16, None,
+                         np.zeros((k.t, k.heads, 64), dtype=U))
+        assert all(np.array_equal(down(o), want) for o in outs[i])
+    both[1].close()
+
+
 @pytest.mark.parametrize("value", [0, 2 ** 64 - 1, 1 << 63, 0x7F7F7F7F7F7F7F7F, 0x8080808080808080])
 def test_words_at_the_ends_of_the_ring(ctx, value):
     """Digits of the largest magnitude over a long contraction: partial sums must not overflow."""
@@ -499,6 +564,11 @@ def test_refusals(ctx):
         with pytest.raises(comet.CometError) as err:
             ctx.attention_scores(**good(**bad))
         assert err.value.code == -1
+    with pytest.raises(comet.CometError) as err:             # no room for a key
+        ctx.attention_weights(0, k.batch, *[torch.zeros((k.t, 4, 0), dtype=torch.int64, device="cuda")] * 4, 0)
+    assert err.value.code == -1
+    need = comet.workspace_bytes(comet.OP_VALUES, 8, 20000, 64, 0)
+    assert need >= 3 * 8 * 64 * 8 and comet.workspace_bytes(comet.OP_SCORES, 8, 64, 20000, 0) == 0
     wide = up(k.words(1, 4098))
     big = torch.zeros((1, 16, 2, 4098), dtype=torch.int64, device="cuda")
     with pytest.raises(comet.CometError) as err:
