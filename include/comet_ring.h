@@ -457,7 +457,7 @@ enum { COMET_CAUSAL = 1 };
  * t(.) the share-local rescaling by frac_bits (0: none).  M_i is the mask under which the scores are sent on (NULL:
  * none).  E, A_i: n_tok x n_heads x d (opened masked queries, and their mask's share); C_i, M_i, Z_i: n_tok x n_heads x
  * ld; pools: n_pages * page_size slots of n_kv_heads x ldp words.
- * d and ldp even, 1 <= d <= ldp, d <= 576; n_kv_heads * ldp < 2^24; ld even, 2 <= ld < 2^24; n_tok * n_heads < 2^31;
+ * d and ldp even, 1 <= d <= ldp, d <= 4096; n_kv_heads * ldp < 2^24; ld even, 2 <= ld < 2^24; n_tok * n_heads < 2^31;
  * n_pages * page_size < 2^31; n_seq * max_q and n_seq * n_kv_heads < 2^24.
  * Z_i may be C_i or M_i; it must not overlap anything else.
  * ws: comet_workspace_bytes(COMET_OP_SCORES, n_tok * n_heads, d, ld, 0) bytes (0: none). */

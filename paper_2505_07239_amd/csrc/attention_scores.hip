@@ -67,8 +67,8 @@ __device__ __forceinline__ void write_out(const ProductParams& p, const RowTile<
 
 // KT: blocks of 64 words that fit the rows' place in LDS.  NT: threads.
 template <int RF, int KT, int NT>
-__global__ __launch_bounds__(NT, RF == 1 && KT <= 8 ? 4 : 2) void scores_kernel(ProductParams p) {
-    constexpr int R = 16 * RF, W = NT / 64, AHEAD = KT > 8 ? 2 : 1;
+__global__ __launch_bounds__(NT, RF == 1 ? 4 : 2) void scores_kernel(ProductParams p) {
+    constexpr int R = 16 * RF, W = NT / 64;
     __shared__ __align__(16) unsigned char rows[KT * R * 512];
     __shared__ RowTile<R> tile;
     const Batch& b = p.b;
@@ -112,9 +112,8 @@ __global__ __launch_bounds__(NT, RF == 1 && KT <= 8 ? 4 : 2) void scores_kernel(
 
     int key0 = first + 16 * wave;
     size_t off = key0 < end ? locate(key0) : 0;
-    u64x2 w[AHEAD][8];
-#pragma unroll
-    for (int n = 0; n < AHEAD; ++n) load(off, n, w[n]);       // (there are two blocks at least)
+    u64x2 w[8];
+    load(off, 0, w);
     // the rows' digits: block kb, digit t, lane group g, row
     auto fetch_rows = [&](int i, u64x2 (&w)[8]) {
         const int kb = i / RF, row = tile.row[(i % RF) * 16 + r];
@@ -150,17 +149,13 @@ __global__ __launch_bounds__(NT, RF == 1 && KT <= 8 ? 4 : 2) void scores_kernel(
         for (int i = 0; i < RF; ++i)
 #pragma unroll
             for (int s = 0; s < 8; ++s) acc[i][s] = v4i{0, 0, 0, 0};
-        for (int kb0 = 0; kb0 < blocks; kb0 += AHEAD) {       // (blocks is even, AHEAD one or two)
-#pragma unroll
-            for (int n = 0; n < AHEAD; ++n) {
-                v4i f[8];
-                to_units(w[n], f);
-                __builtin_amdgcn_sched_barrier(0);
-                const int kb = kb0 + n, then = kb + AHEAD;
-                const bool over = then >= blocks;
-                load(over ? off_next : off, over ? then - blocks : then, w[n]);
-                multiply_block<RF>(acc, f, mine + (size_t)kb * (R * 512));
-            }
+        for (int kb = 0; kb < blocks; ++kb) {
+            v4i f[8];
+            to_units(w, f);
+            __builtin_amdgcn_sched_barrier(0);
+            const bool last = kb + 1 == blocks;
+            load(last ? off_next : off, last ? 0 : kb + 1, w);
+            multiply_block<RF>(acc, f, mine + (size_t)kb * (R * 512));
         }
         off = off_next;
         write_out<RF>(p, tile, acc, key0, lane);
@@ -188,9 +183,9 @@ struct Source {
     }
 };
 
-// Rows whose digits do not fit LDS: 16 RF rows x 128 keys, the contraction streamed (sweep_blocks).
-template <int RF>
-__global__ __launch_bounds__(512) void scores_many_kernel(ProductParams p) {
+// Rows whose digits do not fit LDS: 16 RF rows x 16 W keys, the contraction streamed (sweep_blocks).
+template <int RF, int W>
+__global__ __launch_bounds__(64 * W) void scores_many_kernel(ProductParams p) {
     constexpr int R = 16 * RF, HALF = R * 512;
     __shared__ __align__(16) unsigned char stage[4 * HALF];
     __shared__ RowTile<R> tile;
@@ -208,7 +203,7 @@ __global__ __launch_bounds__(512) void scores_many_kernel(ProductParams p) {
 
     const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-    const int key0 = unit.chunk * p.chunk + 16 * wave;        // (a chunk is 128 keys)
+    const int key0 = unit.chunk * p.chunk + 16 * wave;        // (a chunk is 16 W keys)
     const bool works = key0 < most, feeds = wave < 2 * RF;
     const int ch = (wave / RF) & 1, cr = (wave % RF) * 16 + r, row = tile.row[cr] < 0 ? 0 : tile.row[cr];
     const u32 row_bytes = (u32)(b.n_kv_heads * p.ldp) * 8u, head_at = (u32)(unit.kvh * p.ldp) * 8u;
@@ -248,18 +243,22 @@ int comet_attn::launch_scores(comet_ctx* ctx, const char* what, ProductParams& p
     int R, W;
     void (*kern)(ProductParams);
     const int64_t pairs = (int64_t)b.n_seq * b.n_kv_heads;
-    // The streamed kernel reads keys once for 64 rows instead of 16, but starts slowly: for long contractions, when there are
-    // workgroups for every compute unit (d = 576, 37 tokens of 64 heads over 2037 keys: 807 -> 270 us; one token of 64 heads of
-    // 4 sequences: 64 us here and 88 streamed; d = 192: 117 here and 173).
-    const bool many = n_rows > 16 && blocks > 8 && pairs * ((n_rows + 63) / 64) * ((b.kv_cap + 127) / 128) >= ctx->num_cu;
-    if (many) { kern = n_rows > 32 ? scores_many_kernel<4> : scores_many_kernel<2>; R = n_rows > 32 ? 64 : 32; W = 8; }
+    // d > 256: the rows' digits would fill LDS (and 16 rows of them would leave one workgroup on a compute unit): the contraction is
+    // streamed, with tiles of 64 x 128 where there is one for every compute unit, smaller ones, of which a compute unit holds several,
+    // below.  576 words: 37 tokens of 64 heads over 2037 keys 273 us (32 x 64: 313; resident rows 807), one token of 64 heads of 4
+    // sequences of 4000 keys 69 us (64 x 128: 131), of 16 heads 39 us (resident 64).
+    // d <= 256: resident rows (192 words, 512 tokens of 32 heads: 115 us, streamed 197; d = 128: 151 and 172).
+    if (blocks > 8) {
+        const bool large = n_rows > 32 && pairs * ((n_rows + 63) / 64) * ((b.kv_cap + 127) / 128) >= ctx->num_cu;
+        if (large) { kern = scores_many_kernel<4, 8>; R = 64; W = 8; }
+        else { kern = n_rows > 16 ? scores_many_kernel<2, 4> : scores_many_kernel<1, 4>; R = n_rows > 16 ? 32 : 16; W = 4; }
+    }
     else if (n_rows > 32 && blocks <= 2) { kern = scores_kernel<4, 2, 256>; R = 64; W = 4; }
     else if (n_rows > 32 && blocks <= 4) { kern = scores_kernel<4, 4, 512>; R = 64; W = 8; }
     else if (n_rows > 16 && blocks <= 4) { kern = scores_kernel<2, 4, 256>; R = 32; W = 4; }
-    else if (n_rows > 16 && blocks <= 8) { kern = scores_kernel<2, 8, 512>; R = 32; W = 8; }
+    else if (n_rows > 16) { kern = scores_kernel<2, 8, 512>; R = 32; W = 8; }
     else if (blocks <= 4) { kern = scores_kernel<1, 4, 256>; R = 16; W = 4; }
-    else if (blocks <= 8) { kern = scores_kernel<1, 8, 512>; R = 16; W = 8; }
-    else { kern = scores_kernel<1, 18, 768>; R = 16; W = 12; }
+    else { kern = scores_kernel<1, 8, 512>; R = 16; W = 8; }
     p.tiles = (int)((n_rows + R - 1) / R);
     const int64_t tokens = R / b.group + 2 < b.max_q ? R / b.group + 2 : b.max_q;    // that a tile of rows may touch
     p.far_rows = tokens * b.n_heads * b.ld * 8 >= 0x7fffffffll;
@@ -268,7 +267,7 @@ int comet_attn::launch_scores(comet_ctx* ctx, const char* what, ProductParams& p
     const int64_t units = pairs * p.tiles, wanted = (blocks <= 4 && R == 16 ? 32ll : 2ll) * ctx->num_cu;
     int64_t chunks = (wanted + units - 1) / units;
     const int64_t most = (b.kv_cap + 16 * W - 1) / (16 * W);
-    if (chunks > most || many) chunks = most;
+    if (chunks > most || blocks > 8) chunks = most;
     if (chunks < 1) chunks = 1;
     p.chunk = (int)(((b.kv_cap + chunks - 1) / chunks + 16 * W - 1) / (16 * W) * (16 * W));
     p.chunks = (b.kv_cap + p.chunk - 1) / p.chunk;

@@ -253,6 +253,6 @@ int launch_scores(comet_ctx* ctx, const char* what, ProductParams& p);
 int launch_values(comet_ctx* ctx, const char* what, ProductParams& p, void* ws, size_t ws_bytes);
 size_t values_workspace_bytes(int64_t m, int64_t ld, int64_t d);
 
-constexpr int MAX_D = 576;       // words of a cached row that a product contracts, or of a row of values
+constexpr int MAX_D = 4096;      // words of a cached row that a product contracts (an int32 plane takes 8191), or of a row of values
 
 }  // namespace comet_attn

@@ -135,7 +135,7 @@ def test_products(ctx, n, d, ldp):
     check_values(ctx, k, d, 1 - party, 13, n % 3 != 1)
 
 
-@pytest.mark.parametrize("d,ldp,heads", [(576, 576, 16), (576, 576, 70), (512, 576, 16), (512, 576, 70), (322, 324, 3)])
+@pytest.mark.parametrize("d,ldp,heads", [(576, 576, 16), (576, 576, 70), (512, 576, 16), (512, 576, 70), (322, 324, 3), (1000, 1002, 18), (4096, 4096, 2)])
 def test_latent_rows(ctx, d, ldp, heads):
     """One row a token for all query heads; the values are the first words of the keys' rows."""
     say("latent d=%d ldp=%d heads=%d" % (d, ldp, heads))
