@@ -1,12 +1,22 @@
 // Queries times cached keys (comet_attention_scores) on the int8 matrix cores:
 //     Z(r, j) = t(C(r, j) + [E | A](r, :) . [X | F](j, :)) - M(r, j).
 //
-// A workgroup holds R = 16 RF rows in LDS, as digits, for the whole stacked contraction (E and A, each filled up to whole blocks of 64 words); behind
-// the barrier that follows, its wavefronts are on their own.  Each takes every W-th tile of 16 keys: it loads its keys' words
-// straight into registers, a block of 64 words ahead of their use, splits them into digits and transposes them there (no
-// other wavefront of the workgroup wants them), and multiplies them with the rows' digits, read from LDS in operand
-// order.  So a cached word is fetched once per row tile, a query word once per workgroup, and while one
-// wavefront of a SIMD writes its tile out the other multiplies.
+// scores_kernel, d <= 256: a workgroup holds R = 16 RF rows in LDS, as digits, for the whole stacked contraction (E and A, each
+// filled up to whole blocks of 64 words); behind the barrier that follows, its wavefronts are on their own.  Each takes every
+// W-th tile of 16 keys: it loads its keys' words straight into registers, a block ahead of their use, splits them into
+// digits and transposes them there (no other wavefront of the workgroup wants them), and multiplies them with the rows'
+// digits, read from LDS in operand order.  So a cached word is fetched once per row tile, a query word once per workgroup.
+// scores_many_kernel, d > 256: the rows' digits would not fit; both sides are streamed (sweep_blocks in attention_tile.h).
+//
+// What bounds them (us of a call; the floor at 5.9 TB/s and 3.9 POP/s):
+//   * few rows, the cache read once: HBM.  16 sequences of up to 8193 keys, 8 key heads of 128 words, 4 rows each: 280 (floor 262,
+//     5.5 TB/s).  Loads past the caches are slower here (374): a load takes half a line, the next one the other half.
+//   * prompts, 4 of up to 512 tokens, 32 heads of 128: 153 (floor 75, matrix units busy 31 %).  By time stamps a workgroup of 64 rows
+//     takes 7 us to begin (its row's digits 5), then per tile and pair of wavefronts 10 us of multiplying, in which the matrix units
+//     are busy for nine tenths, and 7 of writing out, in which they are not.  Tried, without gain: 32 and 48 rows, more
+//     workgroups of fewer rows or keys, C and M requested early (registers, or their lines into L2), priorities.
+//   * latent rows, 64 heads of 4 sequences over 576 words: 62 (floor 22): a chain of nine blocks whose loads one wavefront per SIMD
+//     cannot cover; smaller tiles that would add wavefronts split the keys more often (85).
 #include "attention_tile.h"
 
 using namespace comet_attn;

@@ -4,12 +4,16 @@
 // The contraction runs over the keys, in blocks of 64, for E X and A F in turn.  A lane loads the sixteen words of
 // its column in sixteen cached rows (consecutive lanes read consecutive columns) and of its row of weights, and splits and
 // transposes both in registers.  Two kernels:
-//   * values_few_kernel, up to 16 rows (a decoding step): bound by reading the cache once.  A wavefront has 16 rows x 64
-//     columns and every eighth block of keys; nothing is shared, so there is no barrier until the eight wavefronts of a
-//     workgroup add their sums up in LDS.
-//   * values_many_kernel: 16 RF rows x 128 columns.  A wavefront has 16 columns, whose cached words only it reads; the
+//   * values_few_kernel, up to 16 rows (a decoding step): a wavefront has 16 rows x 16 CT columns and every eighth block of
+//     keys; nothing is shared, so there is no barrier until the eight wavefronts of a workgroup add their sums up in LDS.
+//     Bound by HBM: 16 sequences of up to 8193 keys, 8 key heads of 128 words, 4 rows each: 288 us (floor 258 at 5.9 TB/s; 311 without
+//     loads past the caches).  One token of 12 heads of 64 over 201 keys: 5.9 us, a chain of six dependent loads.
+//   * values_many_kernel: 16 RF rows x 16 COLW columns.  A wavefront has 16 columns, whose cached words only it reads; the
 //     weights, which all of them need, are converted once by all threads into one of two LDS stages while the other is
-//     multiplied.  With at most 64 columns four wavefronts take E X and four A F.
+//     multiplied (sweep_blocks in attention_tile.h).  With at most 64 columns four wavefronts take E X and four A F.
+//     Bound by the matrix units and power: 512 tokens of 32 heads over 4608 keys, 560 us (floor 337 at 3.9 POP/s of random
+//     operands), matrix units busy 59 % of the cycles at 1.87 GHz.  With 48 rows 648, with the two wavefronts of a SIMD in step
+//     and 64 rows 830; a barrier that waits for memory, or a spilled register in the loop, costs as much.
 // Long sequences with few rows are cut into pieces, whose sums (of words, so that their order changes nothing)
 // values_finish_kernel adds up.
 #include "attention_tile.h"

