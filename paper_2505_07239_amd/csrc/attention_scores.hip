@@ -89,13 +89,9 @@ __global__ __launch_bounds__(NT, RF == 1 ? 4 : 2) void scores_kernel(ProductPara
     const int rt = p.tiles - 1 - unit.inner;       // (the rows that see most come first)
     const int r0 = rt * R;
     if (r0 >= sq.nq * b.group) return;
-    tile.fill(b, sq, kvh, r0);
-    __syncthreads();
-    int most, least;
-    tile.span(most, least);
     const int first = unit.chunk * p.chunk;
-    const int end = most < first + p.chunk ? most : first + p.chunk;
-    if (first >= end) return;
+    if (first >= sq.kv) return;
+    tile.fill(b, sq, kvh, r0);
 
     const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
@@ -121,9 +117,14 @@ __global__ __launch_bounds__(NT, RF == 1 ? 4 : 2) void scores_kernel(ProductPara
     };
 
     int key0 = first + 16 * wave;
-    size_t off = key0 < end ? locate(key0) : 0;
+    size_t off = key0 < sq.kv ? locate(key0) : 0;
     u64x2 w[8];
-    load(off, 0, w);
+    load(off, 0, w);                                          // (under way while the rest is found out)
+    __syncthreads();
+    int most, least;
+    tile.span(most, least);
+    const int end = most < first + p.chunk ? most : first + p.chunk;
+    if (first >= end) return;
     // the rows' digits: block kb, digit t, lane group g, row
     auto fetch_rows = [&](int i, u64x2 (&w)[8]) {
         const int kb = i / RF, row = tile.row[(i % RF) * 16 + r];
