@@ -27,13 +27,15 @@ template <int T>
 __global__ __launch_bounds__(T < 256 ? 256 : T) void weights_kernel(WeightParams p, int n_rows) {
     constexpr int NT = T < 256 ? 256 : T, U = 2;
     const Batch& b = p.b;
-    const int place = (int)blockIdx.x * (NT / T) + (int)threadIdx.x / T, lane = (int)threadIdx.x % T;
-    const bool inside = place < n_rows;
-    const unsigned w = inside ? (unsigned)place : 0;
-    const int h = (int)(w % (unsigned)b.n_heads);
-    const int j = (int)(w / (unsigned)b.n_heads % (unsigned)b.max_q);
-    const Sequence sq(b, (int)(w / (unsigned)b.n_heads / (unsigned)b.max_q));
-    const bool live = inside && j < sq.nq;
+    const unsigned at = (b.block0 + blockIdx.x) * (unsigned)(NT / T) + threadIdx.x / T;
+    const int lane = (int)threadIdx.x % T;
+    const bool inside = at < (unsigned)n_rows;
+    const unsigned w = inside ? at / (unsigned)b.n_heads : 0;
+    const int h = inside ? (int)(at % (unsigned)b.n_heads) : 0;
+    const Place place(b, w);
+    const Sequence sq(b, place.s);
+    const int j = place.of(b, sq, w);
+    const bool live = inside && j >= 0;
     const int v = live ? sq.sees(b, j, h) : 0;
     const size_t row = (size_t)(sq.q0 + (live ? j : 0)) * b.n_heads + h, base = row * b.ld;
     u64 sum = 0;
@@ -116,8 +118,10 @@ int make_product(comet_ctx* ctx, const char* what, int party, const comet_kv_bat
         return comet_fail(ctx, COMET_ECAP, "%s: d must be at most %d, a slot's words below 2^24", what, MAX_D);
     if (p->b.n_tok == 0 || p->b.n_seq == 0 || p->b.max_q == 0) return COMET_OK;
     if (n_pages < 1 && p->b.kv_cap > 0) return comet_fail(ctx, COMET_EINVAL, "%s: empty pools", what);
-    const void* ptrs[] = {E, A_i, f_pool, x_pool, C_i, Z_i};
-    for (const void* q : ptrs) {
+    // (no pool is read where a sequence has no pages)
+    const void* ptrs[] = {E, A_i, C_i, Z_i, f_pool, x_pool};
+    for (int i = 0; i < (p->b.kv_cap > 0 ? 6 : 4); ++i) {
+        const void* const q = ptrs[i];
         if (!q) return comet_fail(ctx, COMET_EINVAL, "%s: null pointer", what);
         if (!comet_aligned16(q)) return comet_fail(ctx, COMET_EALIGN, "%s: operands must be 16-byte aligned", what);
     }
@@ -193,17 +197,11 @@ int comet_attention_weights(comet_ctx* ctx, int party, const comet_kv_batch* bat
     p.party = party; p.frac = frac_bits; p.bias = bias;
     p.d0 = (const u64*)d_0; p.d1 = (const u64*)d_1; p.r = (const u64*)r_i; p.r2 = (const u64*)r2_i; p.m = (const u64*)m_i;
     p.out = (u64*)out; p.sums = (u64*)sums;
-    const int64_t n_rows = (int64_t)b.n_seq * b.max_q * b.n_heads;
-    if (n_rows > 0x7fffffffll) return comet_fail(ctx, COMET_ECAP, "%s: too many rows", what);
+    const int n_rows = (int)(Place::count(b) * b.n_heads);    // (at most n_tok * n_heads)
     // A wavefront per row where rows are short (prompts: many rows), a whole workgroup of sixteen where they are long and few.
-    if (b.kv_cap <= 1024)
-        hipLaunchKernelGGL(weights_kernel<64>, dim3((unsigned)((n_rows + 3) / 4)), dim3(256), 0, ctx->stream, p, (int)n_rows);
-    else if (b.kv_cap <= 4096)
-        hipLaunchKernelGGL(weights_kernel<256>, dim3((unsigned)n_rows), dim3(256), 0, ctx->stream, p, (int)n_rows);
-    else
-        hipLaunchKernelGGL(weights_kernel<1024>, dim3((unsigned)n_rows), dim3(1024), 0, ctx->stream, p, (int)n_rows);
-    COMET_LAUNCH_CHECK(ctx, what);
-    return COMET_OK;
+    if (b.kv_cap <= 1024) return launch_all(ctx, what, weights_kernel<64>, ((int64_t)n_rows + 3) / 4, 256, p, n_rows);
+    if (b.kv_cap <= 4096) return launch_all(ctx, what, weights_kernel<256>, n_rows, 256, p, n_rows);
+    return launch_all(ctx, what, weights_kernel<1024>, n_rows, 1024, p, n_rows);
 }
 
 }  // extern "C"

@@ -284,8 +284,5 @@ int comet_attn::launch_scores(comet_ctx* ctx, const char* what, ProductParams& p
     p.chunks = (b.kv_cap + p.chunk - 1) / p.chunk;
     p.parts = Unit::parts(b, p.chunks);
     const int64_t grid = Unit::grid(b, p.tiles, p.chunks, p.parts);
-    if (grid > 0x7fffffffll) return comet_fail(ctx, COMET_ECAP, "%s: too many rows", what);
-    hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(64 * W), 0, ctx->stream, p);
-    COMET_LAUNCH_CHECK(ctx, what);
-    return COMET_OK;
+    return launch_all(ctx, what, kern, grid, 64 * W, p);
 }

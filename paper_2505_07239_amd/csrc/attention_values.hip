@@ -267,13 +267,13 @@ __global__ __launch_bounds__(NT) void values_many_kernel(ProductParams p) {
 // Adds up the pieces of a row that have been written: those that begin before the last key it sees, and the first.
 __global__ __launch_bounds__(256) void values_finish_kernel(ProductParams p, int pieces) {
     const Batch& b = p.b;
-    unsigned w = blockIdx.x;
+    unsigned w = b.block0 + blockIdx.x;
     const int piece = (int)(w % (unsigned)pieces); w /= (unsigned)pieces;
     const int h = (int)(w % (unsigned)b.n_heads); w /= (unsigned)b.n_heads;
-    const int j = (int)(w % (unsigned)b.max_q);
-    const Sequence sq(b, (int)(w / (unsigned)b.max_q));
-    const int col = piece * 256 + threadIdx.x;
-    if (j >= sq.nq || col >= p.d) return;
+    const Place place(b, w);
+    const Sequence sq(b, place.s);
+    const int j = place.of(b, sq, w), col = piece * 256 + threadIdx.x;
+    if (j < 0 || col >= p.d) return;
     const int row = (sq.q0 + j) * b.n_heads + h, sees = sq.sees(b, j, h);
     const size_t all = (size_t)b.n_tok * b.n_heads * p.d;
     const u64* from = p.part + (size_t)row * p.d + col;
@@ -341,13 +341,8 @@ int comet_attn::launch_values(comet_ctx* ctx, const char* what, ProductParams& p
     p.parts = Unit::parts(b, p.chunks);
     const int64_t grid = Unit::grid(b, (int64_t)p.tiles * p.groups, p.chunks, p.parts);
     const int pieces = (p.d + 255) / 256;
-    const int64_t finish = (int64_t)b.n_seq * b.max_q * b.n_heads * pieces;
-    if (grid > 0x7fffffffll || finish > 0x7fffffffll) return comet_fail(ctx, COMET_ECAP, "%s: too many rows", what);
-    hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(NT), 0, ctx->stream, p);
-    COMET_LAUNCH_CHECK(ctx, what);
-    if (p.part) {
-        hipLaunchKernelGGL(values_finish_kernel, dim3((unsigned)finish), dim3(256), 0, ctx->stream, p, pieces);
-        COMET_LAUNCH_CHECK(ctx, what);
-    }
-    return COMET_OK;
+    const int64_t finish = Place::count(b) * b.n_heads * pieces;
+    if (finish > 0x7fffffffll) return comet_fail(ctx, COMET_ECAP, "%s: too many rows", what);
+    const int rc = launch_all(ctx, what, kern, grid, NT, p);
+    return rc != COMET_OK || !p.part ? rc : launch_all(ctx, what, values_finish_kernel, finish, 256, p, pieces);
 }

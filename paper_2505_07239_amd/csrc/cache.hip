@@ -140,10 +140,12 @@ __global__ __launch_bounds__(GT) void rotate_kernel(RotateParams p, int pieces) 
     }
 }
 
-// workgroups that share a row of n units
-inline int row_pieces(int64_t n, int per_thread) {
+// workgroups that share a row of n units (a launch has fewer than 2^32 threads: 2^24 workgroups)
+inline int row_pieces(int64_t n_tok, int64_t n, int per_thread) {
     int64_t g = (n + (int64_t)GT * per_thread - 1) / ((int64_t)GT * per_thread);
-    return (int)(g < 1 ? 1 : g > 64 ? 64 : g);
+    if (g > 64) g = 64;
+    if (g * n_tok > COMET_DIM_MAX) g = COMET_DIM_MAX / n_tok;
+    return (int)(g < 1 ? 1 : g);
 }
 
 // lanes of a row, as a power of two: a whole workgroup (8) for rows of more than 128 vectors
@@ -153,7 +155,7 @@ inline int row_log(int64_t n) {
     return log;
 }
 inline unsigned row_grid(int64_t n_tok, int pieces, int log) {
-    return (unsigned)(log < 8 ? (n_tok + (GT >> log) - 1) >> (8 - log) : n_tok * pieces);   // n_tok < 2^24, pieces <= 64
+    return (unsigned)(log < 8 ? (n_tok + (GT >> log) - 1) >> (8 - log) : n_tok * pieces);
 }
 
 int check_rows(comet_ctx* ctx, const char* what, int party, const void* const (&ptrs)[5], const int32_t* slots, int64_t n_tok,
@@ -184,7 +186,7 @@ int comet_cache_write(comet_ctx* ctx, int party, const uint64_t* d_0, const uint
     comet_device_guard guard(ctx);
     if (!guard.ok) return comet_fail(ctx, COMET_EDEVICE, "%s: cannot select device", what);
     const bool vec = (width & 1) == 0;
-    const int nvec = (int)(vec ? width / 2 : width), pieces = row_pieces(nvec, 2), log = row_log(nvec);
+    const int nvec = (int)(vec ? width / 2 : width), pieces = row_pieces(n_tok, nvec, 2), log = row_log(nvec);
     const dim3 grid(row_grid(n_tok, pieces, log));
     auto kern = vec ? cache_write_kernel<2> : cache_write_kernel<1>;
     hipLaunchKernelGGL(kern, grid, dim3(GT), 0, ctx->stream, party, (const u64*)d_0, (const u64*)d_1, (const u64*)b_i, slots,
@@ -202,7 +204,7 @@ int comet_cache_read(comet_ctx* ctx, int party, const uint64_t* f_pool, const ui
     comet_device_guard guard(ctx);
     if (!guard.ok) return comet_fail(ctx, COMET_EDEVICE, "%s: cannot select device", what);
     const bool vec = (width & 1) == 0;
-    const int nvec = (int)(vec ? width / 2 : width), pieces = row_pieces(nvec, 2), log = row_log(nvec);
+    const int nvec = (int)(vec ? width / 2 : width), pieces = row_pieces(n_tok, nvec, 2), log = row_log(nvec);
     const dim3 grid(row_grid(n_tok, pieces, log));
     auto kern = vec ? cache_read_kernel<2> : cache_read_kernel<1>;
     hipLaunchKernelGGL(kern, grid, dim3(GT), 0, ctx->stream, party, (const u64*)f_pool, (const u64*)x_pool, slots,
@@ -241,7 +243,7 @@ int comet_rotate_share(comet_ctx* ctx, int party, const uint64_t* x_i, int64_t l
     // two words at a time where every vector of a head, of the table and of x_i starts on 16 bytes
     const bool vec = (head_dim & 1) == 0 && (p.half & 1) == 0 && (ldx & 1) == 0 && comet_aligned16(x_i);
     p.units = n_heads * (head_dim - p.half) / (vec ? 2 : 1);
-    const int pieces = row_pieces(p.units, 1);
+    const int pieces = row_pieces(n_tok, p.units, 1);
     auto kern = vec ? (p.interleaved ? rotate_kernel<2, true> : rotate_kernel<2, false>)
                     : (p.interleaved ? rotate_kernel<1, true> : rotate_kernel<1, false>);
     hipLaunchKernelGGL(kern, dim3((unsigned)(n_tok * pieces)), dim3(GT), 0, ctx->stream, p, pieces);

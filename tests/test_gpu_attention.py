@@ -189,6 +189,80 @@ def test_rows_far_apart(ctx):
     assert np.array_equal(down(got), oa.values(0, rows, want, m, f, x, np.array([[2, 0, 1, 3]]), z, 16, None, np.zeros_like(z)))
 
 
+def test_more_workgroups_than_one_launch_takes(ctx):
+    """A bound on a sequence's tokens that one prompt could fill, for many sequences: more than 2^32 threads."""
+    say("many workgroups")
+    import paper_2505_07239_amd as comet
+    n_seq, t, heads, page, d, new = 1100, 1030, 128, 1024, 320, 9
+    q_start, kv_len = np.zeros(n_seq + 1, dtype=np.int32), np.zeros(n_seq, dtype=np.int32)
+    q_start[1:], q_start[601:], q_start[1100:] = 3, 8, 9
+    kv_len[0], kv_len[600], kv_len[1099] = 40, 5, 150
+    table = np.arange(n_seq, dtype=np.int32).reshape(n_seq, 1) % 3
+    table[600], table[1099] = 2, 1
+    batch = comet.KVBatch(t, heads, 1, ints(q_start), ints(kv_len), ints(table), page, t)
+    rows = list(oa.rows(q_start, kv_len, heads))
+    f, x = u64(2300, 1, 3, page, 1, 512), u64(2300, 2, 3, page, 1, 512)
+
+    def wide(stream, last):
+        """[t, heads, last] words, random for the tokens of the batch, the pattern behind them."""
+        small = pattern(new, heads, last) if stream is None else u64(2300, stream, new, heads, last)
+        all_of = torch.full((t, heads, last), PATTERN, dtype=torch.int64, device="cuda")
+        all_of[:new] = up(small)
+        return small, all_of
+
+    def same(got, want):
+        assert np.array_equal(down(got[:new].contiguous()), want)
+        assert bool((got[new:] == PATTERN).all())
+
+    (e, e_), (a, a_), (c, c_), (z, z_) = wide(3, d), wide(4, d), wide(5, page), wide(None, page)
+    same(ctx.attention_scores(1, batch, e_, a_, up(f), up(x), c_, 16, out=z_), oa.scores(1, rows, e, a, f, x, table, c, 16, None, z))
+    (w, w_), (v, v_), (c, c_), (z, z_) = wide(6, page), wide(7, page), wide(8, 512), wide(None, 512)
+    same(ctx.attention_values(0, batch, w_, v_, up(f), up(x), c_, 16, out=z_), oa.values(0, rows, w, v, f, x, table, c, 16, None, z))
+    (z, z_), (sums, sums_) = wide(None, page), wide(None, 1)
+    got = ctx.attention_weights(1, batch, w_, None, v_, w_, 5, 16, out=(z_, sums_[:, :, 0].contiguous()))
+    want = oa.weights(1, rows, w, None, v, w, 5, 16, None, z, sums[:, :, 0])
+    same(got[0], want[0]), same(got[1], want[1])
+
+
+def test_more_rows_of_weights_than_one_launch_takes(ctx):
+    say("many rows")
+    import paper_2505_07239_amd as comet
+    t, heads = (1 << 19) + 5, 128
+    batch = comet.KVBatch(t, heads, 1, ints([0, t]), ints([2]), ints([[0]]), 16, t, causal=False)
+    gen = torch.Generator(device="cuda").manual_seed(2310)
+    u, r, r2 = (torch.randint(-2 ** 63, 2 ** 63 - 1, (t, heads, 2), dtype=torch.int64, device="cuda", generator=gen) for _ in range(3))
+    out, sums = ctx.attention_weights(0, batch, u, None, r, r2, 3, 7)
+    want = (r2 + 2 * (u + 3) * r) >> 7
+    assert torch.equal(out, want) and torch.equal(sums, want[:, :, 0] + want[:, :, 1])
+
+
+@pytest.mark.parametrize("lens,max_q", [([(9, 30), (1, 3), (0, 4), (2, 8)], 4), ([(1, 900), (0, 0), (0, 7), (40, 700), (1, 1), (0, 9)], None),
+                                        ([(0, 3), (30, 30)] + [(1, 20 * s) for s in range(20)], None)])
+@pytest.mark.parametrize("heads,kvh", [(4, 2), (40, 1)])
+def test_prompts_among_single_tokens(ctx, lens, max_q, heads, kvh):
+    say("mixed %s heads=%d" % (lens, heads))
+    k = Case(2320 + len(lens) + heads, lens, heads, kvh, ldp=80, gap=2, pad=3, max_q=max_q, spare=20)
+    check_weights(ctx, k, 1, 16, True, False)
+    check_scores(ctx, k, 80, 0, 16, True)
+    check_values(ctx, k, 80, 1, 16, True)
+
+
+@pytest.mark.parametrize("new", [1, 30])
+def test_no_pages(ctx, new):
+    """A cache without pages: no row sees anything, the values are what their masks say."""
+    say("no pages")
+    import paper_2505_07239_amd as comet
+    t, heads, d, ld = 2 * new, 2, 6, 16
+    batch = comet.KVBatch(t, heads, 1, ints([0, new, t]), ints([3, 0]), torch.zeros((2, 0), dtype=torch.int32, device="cuda"), 16, new)
+    pool = torch.zeros((0, 16, 1, 8), dtype=torch.int64, device="cuda")
+    e, c, m, z = u64(2330, 1, t, heads, ld), u64(2330, 2, t, heads, d), u64(2330, 3, t, heads, d), pattern(t, heads, ld)
+    got = ctx.attention_values(1, batch, up(e), up(e), pool, pool, up(c), 16, up(m))
+    assert np.array_equal(down(got), oa.rescale(1, c, 16) - m)
+    assert np.array_equal(down(ctx.attention_scores(1, batch, up(c), up(c), pool, pool, up(e), 16, out=up(z))), z)
+    w, sums = ctx.attention_weights(0, batch, up(e), None, up(e), up(e), 1, out=(up(z), up(pattern(t, heads))))
+    assert np.array_equal(down(w), z) and not down(sums).any()
+
+
 def test_two_contexts_on_two_streams(ctx):
     """Calls of two contexts in flight together share nothing."""
     import paper_2505_07239_amd as comet
