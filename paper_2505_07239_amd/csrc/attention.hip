@@ -27,7 +27,7 @@ template <int T>
 __global__ __launch_bounds__(T < 256 ? 256 : T) void weights_kernel(WeightParams p, int n_rows) {
     constexpr int NT = T < 256 ? 256 : T, U = 2;
     const Batch& b = p.b;
-    const unsigned at = (b.block0 + blockIdx.x) * (unsigned)(NT / T) + threadIdx.x / T;
+    const unsigned at = block_number() * (unsigned)(NT / T) + __builtin_amdgcn_readfirstlane(threadIdx.x / T);
     const int lane = (int)threadIdx.x % T;
     const bool inside = at < (unsigned)n_rows;
     const unsigned w = inside ? at / (unsigned)b.n_heads : 0;
@@ -99,6 +99,7 @@ int make_batch(comet_ctx* ctx, const char* what, const comet_kv_batch* in, int64
     b->group = in->n_heads / in->n_kv_heads;
     b->page_size = in->page_size; b->max_pages = in->max_pages; b->n_pages = (int)n_pages;
     b->max_q = in->max_q < in->n_tok ? in->max_q : in->n_tok; b->causal = (in->flags & COMET_CAUSAL) != 0;
+    b->by_sequence = Place::by_sequence(*b);
     b->ld = (int)ld;
     const int64_t cap = (int64_t)in->max_pages * in->page_size;
     b->kv_cap = (int)(cap < ld ? cap : ld);
@@ -197,7 +198,7 @@ int comet_attention_weights(comet_ctx* ctx, int party, const comet_kv_batch* bat
     p.party = party; p.frac = frac_bits; p.bias = bias;
     p.d0 = (const u64*)d_0; p.d1 = (const u64*)d_1; p.r = (const u64*)r_i; p.r2 = (const u64*)r2_i; p.m = (const u64*)m_i;
     p.out = (u64*)out; p.sums = (u64*)sums;
-    const int n_rows = (int)(Place::count(b) * b.n_heads);    // (at most n_tok * n_heads)
+    const int n_rows = (int)(Place::count(b) * b.n_heads);    // (< 2^31: by_sequence())
     // A wavefront per row where rows are short (prompts: many rows), a whole workgroup of sixteen where they are long and few.
     if (b.kv_cap <= 1024) return launch_all(ctx, what, weights_kernel<64>, ((int64_t)n_rows + 3) / 4, 256, p, n_rows);
     if (b.kv_cap <= 4096) return launch_all(ctx, what, weights_kernel<256>, n_rows, 256, p, n_rows);

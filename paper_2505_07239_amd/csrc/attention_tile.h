@@ -75,7 +75,7 @@ struct Unit {
     bool live;
     __device__ __forceinline__ Unit(const Batch& b, int n_inner, int chunks, int parts) {
         const unsigned per = ((unsigned)n_inner + parts - 1) / (unsigned)parts;
-        const unsigned block = b.block0 + blockIdx.x, q = block >> 3, group = (q / per) * 8 + (block & 7);
+        const unsigned block = block_number(), q = block >> 3, group = (q / per) * 8 + (block & 7);
         const unsigned piece = group / (unsigned)parts, pair = piece / (unsigned)chunks;
         inner = (int)(q % per * (unsigned)parts + group % (unsigned)parts);
         chunk = (int)(piece % (unsigned)chunks);

@@ -264,12 +264,13 @@ __global__ __launch_bounds__(NT) void values_many_kernel(ProductParams p) {
         }
 }
 
-// Adds up the pieces of a row that have been written: those that begin before the last key it sees, and the first.
-__global__ __launch_bounds__(256) void values_finish_kernel(ProductParams p, int pieces) {
+// n: Place::count().  Adds up the pieces of a row that have been written: those that begin before the last key it sees, and the first.
+__global__ __launch_bounds__(256) void values_finish_kernel(ProductParams p, int pieces, unsigned n) {
     const Batch& b = p.b;
-    unsigned w = b.block0 + blockIdx.x;
+    unsigned w = block_number();
     const int piece = (int)(w % (unsigned)pieces); w /= (unsigned)pieces;
     const int h = (int)(w % (unsigned)b.n_heads); w /= (unsigned)b.n_heads;
+    if (w >= n) return;
     const Place place(b, w);
     const Sequence sq(b, place.s);
     const int j = place.of(b, sq, w), col = piece * 256 + threadIdx.x;
@@ -344,5 +345,5 @@ int comet_attn::launch_values(comet_ctx* ctx, const char* what, ProductParams& p
     const int64_t finish = Place::count(b) * b.n_heads * pieces;
     if (finish > 0x7fffffffll) return comet_fail(ctx, COMET_ECAP, "%s: too many rows", what);
     const int rc = launch_all(ctx, what, kern, grid, NT, p);
-    return rc != COMET_OK || !p.part ? rc : launch_all(ctx, what, values_finish_kernel, finish, 256, p, pieces);
+    return rc != COMET_OK || !p.part ? rc : launch_all(ctx, what, values_finish_kernel, finish, 256, p, pieces, (unsigned)Place::count(b));
 }

@@ -8,9 +8,9 @@ namespace comet_attn {
 struct Batch {
     int n_seq, n_tok, n_heads, n_kv_heads, group;   // group: query heads of a key head
     int page_size, max_pages, n_pages;
-    int max_q, causal;
+    int max_q;
+    bool causal, by_sequence;                       // (by_sequence: Place)
     int ld, kv_cap;                                 // words in a row of a score matrix; longest readable sequence
-    unsigned block0;                                // workgroups of the call in launches before this one (launch_all)
     const int* q_start;
     const int* kv_len;
     const int* block_table;
@@ -51,12 +51,13 @@ struct Sequence {
     }
 };
 
-// Kernels with rows of their own count places (sequence, j < max_q), or tokens where those are fewer: one long prompt among
-// many sequences must not cost as many workgroups as a batch of such prompts.
+// Kernels with rows of their own count places (sequence, j < max_q), or, where less than half of those could be taken, tokens,
+// whose sequence has to be searched for: one long prompt among many sequences must not cost as many workgroups as a batch of
+// such prompts.  (The weights of four prompts of up to 512 tokens: 91 us by places, 93 by tokens.)
 struct Place {
     int s, token;
     __device__ __forceinline__ Place(const Batch& b, unsigned i) {
-        if (by_sequence(b)) {
+        if (b.by_sequence) {
             s = (int)(i / (unsigned)b.max_q);
             token = -1;
             return;
@@ -76,21 +77,23 @@ struct Place {
         const int j = token < 0 ? (int)(i % (unsigned)b.max_q) : token - sq.q0;
         return j >= 0 && j < sq.nq && j < b.max_q ? j : -1;
     }
-    static __host__ __device__ __forceinline__ bool by_sequence(const Batch& b) { return (int64_t)b.n_seq * b.max_q <= b.n_tok; }
-    static int64_t count(const Batch& b) { return by_sequence(b) ? (int64_t)b.n_seq * b.max_q : b.n_tok; }
+    static bool by_sequence(const Batch& b) {
+        const int64_t n = (int64_t)b.n_seq * b.max_q;
+        return n <= 2ll * b.n_tok && n * b.n_heads <= 0x7fffffffll;
+    }
+    static int64_t count(const Batch& b) { return b.by_sequence ? (int64_t)b.n_seq * b.max_q : b.n_tok; }
 };
 
-// A launch has fewer than 2^32 threads; more workgroups than that allows go in several, each a multiple of eight of them, so
-// that the XCDs take turns as in one.
-template <class Params, class... More>
-int launch_all(comet_ctx* ctx, const char* what, void (*kern)(Params, More...), int64_t grid, int threads, Params& p, More... more) {
+// A grid has fewer than 2^32 threads along x; more workgroups than fit get a second axis, with as many as 2^20 - 1 at the end
+// that have nothing to do.  (2^20 is a multiple of eight: the XCDs take turns as along one axis.)
+__device__ __forceinline__ unsigned block_number() { return (blockIdx.y << 20) + blockIdx.x; }
+template <class... Args>
+int launch_all(comet_ctx* ctx, const char* what, void (*kern)(Args...), int64_t grid, int threads, Args... args) {
     if (grid > 0x7fffffffll) return comet_fail(ctx, COMET_ECAP, "%s: too many rows", what);
-    const int64_t most = ((1ll << 32) - 1) / threads / 8 * 8;
-    for (int64_t at = 0; at < grid; at += most) {
-        p.b.block0 = (unsigned)at;
-        hipLaunchKernelGGL(kern, dim3((unsigned)(grid - at < most ? grid - at : most)), dim3(threads), 0, ctx->stream, p, more...);
-        COMET_LAUNCH_CHECK(ctx, what);
-    }
+    const bool one = grid <= 1 << 20;
+    const dim3 blocks(one ? (unsigned)grid : 1u << 20, one ? 1u : (unsigned)((grid + (1 << 20) - 1) >> 20));
+    hipLaunchKernelGGL(kern, blocks, dim3(threads), 0, ctx->stream, args...);
+    COMET_LAUNCH_CHECK(ctx, what);
     return COMET_OK;
 }
 
