@@ -85,6 +85,7 @@ __global__ __launch_bounds__(NT, RF == 1 ? 4 : 2) void scores_kernel(ProductPara
     const Unit unit(b, p.tiles, p.chunks, p.parts);
     if (!unit.live) return;
     const Sequence sq(b, unit.s);
+    if (!p.takes(sq)) return;
     const int kvh = unit.kvh;
     const int rt = p.tiles - 1 - unit.inner;       // (the rows that see most come first)
     const int r0 = rt * R;
@@ -204,6 +205,7 @@ __global__ __launch_bounds__(64 * W) void scores_many_kernel(ProductParams p) {
     const Unit unit(b, p.tiles, p.chunks, p.parts);
     if (!unit.live) return;
     const Sequence sq(b, unit.s);
+    if (!p.takes(sq)) return;
     const int r0 = (p.tiles - 1 - unit.inner) * R;
     if (r0 >= sq.nq * b.group) return;
     tile.fill(b, sq, unit.kvh, r0);
@@ -247,20 +249,20 @@ __global__ __launch_bounds__(64 * W) void scores_many_kernel(ProductParams p) {
 
 }  // namespace
 
-int comet_attn::launch_scores(comet_ctx* ctx, const char* what, ProductParams& p) {
+static int launch_part(comet_ctx* ctx, const char* what, ProductParams& p, int max_q) {
     const Batch& b = p.b;
     const int blocks = (p.d + 63) / 64 * 2;
-    const int64_t n_rows = (int64_t)b.max_q * b.group;
+    const int64_t n_rows = (int64_t)max_q * b.group;
     int R, W;
     void (*kern)(ProductParams);
-    const int64_t pairs = (int64_t)b.n_seq * b.n_kv_heads;
     // d > 256: the rows' digits would fill LDS (and 16 rows of them would leave one workgroup on a compute unit): the contraction is
     // streamed, with tiles of 64 x 128 where there is one for every compute unit, smaller ones, of which a compute unit holds several,
     // below.  576 words: 37 tokens of 64 heads over 2037 keys 273 us (32 x 64: 313; resident rows 807), one token of 64 heads of 4
     // sequences of 4000 keys 69 us (64 x 128: 131), of 16 heads 39 us (resident 64).
     // d <= 256: resident rows (192 words, 512 tokens of 32 heads: 115 us, streamed 197; d = 128: 151 and 172).
     if (blocks > 8) {
-        const bool large = n_rows > 32 && pairs * ((n_rows + 63) / 64) * ((b.kv_cap + 127) / 128) >= ctx->num_cu;
+        p.tiles = (int)((n_rows + 63) / 64);
+        const bool large = n_rows > 32 && filled_tiles(p, 64) * b.n_kv_heads * ((b.kv_cap + 127) / 128) >= ctx->num_cu;
         if (large) { kern = scores_many_kernel<4, 8>; R = 64; W = 8; }
         else { kern = n_rows > 16 ? scores_many_kernel<2, 4> : scores_many_kernel<1, 4>; R = n_rows > 16 ? 32 : 16; W = 4; }
     }
@@ -275,14 +277,18 @@ int comet_attn::launch_scores(comet_ctx* ctx, const char* what, ProductParams& p
     p.far_rows = tokens * b.n_heads * b.ld * 8 >= 0x7fffffffll;
     // Enough workgroups to fill the chip several times over (sequences differ in length), each with a tile of keys per
     // wavefront at least.
-    const int64_t units = pairs * p.tiles, wanted = (blocks <= 4 && R == 16 ? 32ll : 2ll) * ctx->num_cu;
+    const int64_t units = filled_tiles(p, R) * b.n_kv_heads, wanted = (blocks <= 4 && R == 16 ? 32ll : 2ll) * ctx->num_cu;
     int64_t chunks = (wanted + units - 1) / units;
     const int64_t most = (b.kv_cap + 16 * W - 1) / (16 * W);
     if (chunks > most || blocks > 8) chunks = most;
     if (chunks < 1) chunks = 1;
     p.chunk = (int)(((b.kv_cap + chunks - 1) / chunks + 16 * W - 1) / (16 * W) * (16 * W));
     p.chunks = (b.kv_cap + p.chunk - 1) / p.chunk;
-    p.parts = Unit::parts(b, p.chunks);
+    p.parts = Unit::parts(b, p.chunks, p.split < 0);
     const int64_t grid = Unit::grid(b, p.tiles, p.chunks, p.parts);
     return launch_all(ctx, what, kern, grid, 64 * W, p);
+}
+
+int comet_attn::launch_scores(comet_ctx* ctx, const char* what, ProductParams& p) {
+    return launch_split(p, [&](int max_q) { return launch_part(ctx, what, p, max_q); });
 }

@@ -66,7 +66,7 @@ __global__ __launch_bounds__(NT) void values_few_kernel(ProductParams p) {
     const int rt = p.tiles - 1 - unit.inner / p.groups;       // (the rows that see most come first)
     const int cg = unit.inner % p.groups;
     const Sequence sq(b, unit.s);
-    if (rt * R >= sq.nq * b.group) return;
+    if (rt * R >= sq.nq * b.group || !p.takes(sq)) return;
     tile.fill(b, sq, unit.kvh, rt * R);
     const int first = unit.chunk * p.chunk;
     find_slots(slots, b, sq, first, first + p.chunk < sq.kv ? first + p.chunk : sq.kv);
@@ -173,7 +173,7 @@ __global__ __launch_bounds__(NT) void values_many_kernel(ProductParams p) {
     const int rt = p.tiles - 1 - unit.inner / p.groups;       // (the rows that see most come first)
     const int cg = unit.inner % p.groups;
     const Sequence sq(b, unit.s);
-    if (rt * R >= sq.nq * b.group) return;
+    if (rt * R >= sq.nq * b.group || !p.takes(sq)) return;
     tile.fill(b, sq, unit.kvh, rt * R);
     const int first = unit.chunk * p.chunk;
     find_slots(slots, b, sq, first, first + p.chunk < sq.kv ? first + p.chunk : sq.kv);
@@ -274,7 +274,7 @@ __global__ __launch_bounds__(256) void values_finish_kernel(ProductParams p, int
     const Place place(b, w);
     const Sequence sq(b, place.s);
     const int j = place.of(b, sq, w), col = piece * 256 + threadIdx.x;
-    if (j < 0 || col >= p.d) return;
+    if (j < 0 || col >= p.d || !p.takes(sq)) return;
     const int row = (sq.q0 + j) * b.n_heads + h, sees = sq.sees(b, j, h);
     const size_t all = (size_t)b.n_tok * b.n_heads * p.d;
     const u64* from = p.part + (size_t)row * p.d + col;
@@ -286,10 +286,10 @@ __global__ __launch_bounds__(256) void values_finish_kernel(ProductParams p, int
 }
 
 // Pieces that the workspace of a call may hold: as many as a plane needs, and more while the partial sums of all rows
-// stay small (4 M words).
+// stay small (32 M words).
 int64_t max_chunks(int64_t m, int64_t ld, int64_t d) {
     const int64_t needed = (ld + MAX_CHUNK - 1) / MAX_CHUNK;
-    int64_t n = m * d > 0 ? (4ll << 20) / (m * d) : 1;
+    int64_t n = m * d > 0 ? (32ll << 20) / (m * d) : 1;
     if (n > 64) n = 64;
     if (n > (ld + 255) / 256) n = (ld + 255) / 256;
     return n < needed ? needed : n;
@@ -303,14 +303,9 @@ size_t comet_attn::values_workspace_bytes(int64_t m, int64_t ld, int64_t d) {
     return n < 2 ? 0 : (size_t)n * m * d * 8;
 }
 
-int comet_attn::launch_values(comet_ctx* ctx, const char* what, ProductParams& p, void* ws, size_t ws_bytes) {
+static int launch_part(comet_ctx* ctx, const char* what, ProductParams& p, int max_q, void* ws) {
     const Batch& b = p.b;
-    const int64_t n_rows = (int64_t)b.max_q * b.group, m = (int64_t)b.n_tok * b.n_heads;
-    const size_t need = values_workspace_bytes(m, b.ld, p.d);
-    if (need > 0 && (!ws || ws_bytes < need))
-        return comet_fail(ctx, COMET_EWORKSPACE, "%s: needs %zu bytes of workspace", what, need);
-    if (need > 0 && (reinterpret_cast<uintptr_t>(ws) & 255u) != 0)
-        return comet_fail(ctx, COMET_EALIGN, "%s: the workspace must be 256-byte aligned", what);
+    const int64_t n_rows = (int64_t)max_q * b.group, m = (int64_t)b.n_tok * b.n_heads;
     int R, cols, step;
     void (*kern)(ProductParams);
     // Up to 16 rows: four column tiles a wavefront, for whose sake the weights are loaded and split once; one where there are
@@ -325,13 +320,17 @@ int comet_attn::launch_values(comet_ctx* ctx, const char* what, ProductParams& p
     p.tiles = (int)((n_rows + R - 1) / R);
     p.groups = (p.d + cols - 1) / cols;
     // Pieces of the keys: what the longest-working compute unit does, in steps of `step` keys, with two steps for the beginning
-    // and the end of a workgroup and four for the second launch, which more than one piece needs.
-    const int64_t units = (int64_t)b.n_seq * b.n_kv_heads * p.tiles * p.groups;
+    // and the end of a workgroup, four for the second launch, which more than one piece needs, and one for every 2 M words
+    // of partial sums, written and read again.
+    const int64_t units = filled_tiles(p, R) * b.n_kv_heads * p.groups;
     const int64_t cap = max_chunks(m, b.ld, p.d), needed = (b.kv_cap + MAX_CHUNK - 1) / MAX_CHUNK;
     const int64_t steps = (b.kv_cap + step - 1) / step;
+    const int64_t rows = filled_tiles(p, R) * R * b.n_kv_heads, words = (rows < m ? rows : m) * p.d;
     int64_t chunks = 1, best = INT64_MAX;
     for (int64_t n = needed > 1 ? needed : 1; n <= cap && (n <= steps || n <= needed); ++n) {
-        const int64_t cost = (units * n + ctx->num_cu - 1) / ctx->num_cu * ((steps + n - 1) / n + 2) + (n > 1 ? 4 : 0);
+        // (the units of a mixed batch's prompts are a guess, not worth cutting for the last round of workgroups)
+        if (p.split < 0 && n > needed && units * (n - 1) >= ctx->num_cu) break;
+        const int64_t cost = (units * n + ctx->num_cu - 1) / ctx->num_cu * ((steps + n - 1) / n + 2) + (n > 1 ? 4 + n * words / (2 << 20) : 0);
         if (cost < best) { best = cost; chunks = n; }
     }
     p.chunk = (int)(((b.kv_cap + chunks - 1) / chunks + 63) / 64 * 64);
@@ -339,11 +338,20 @@ int comet_attn::launch_values(comet_ctx* ctx, const char* what, ProductParams& p
     if (p.chunk < 64) p.chunk = 64;
     p.chunks = b.kv_cap > 0 ? (b.kv_cap + p.chunk - 1) / p.chunk : 1;
     p.part = p.chunks > 1 ? (u64*)ws : nullptr;
-    p.parts = Unit::parts(b, p.chunks);
+    p.parts = Unit::parts(b, p.chunks, p.split < 0);
     const int64_t grid = Unit::grid(b, (int64_t)p.tiles * p.groups, p.chunks, p.parts);
     const int pieces = (p.d + 255) / 256;
     const int64_t finish = Place::count(b) * b.n_heads * pieces;
     if (finish > 0x7fffffffll) return comet_fail(ctx, COMET_ECAP, "%s: too many rows", what);
     const int rc = launch_all(ctx, what, kern, grid, NT, p);
     return rc != COMET_OK || !p.part ? rc : launch_all(ctx, what, values_finish_kernel, finish, 256, p, pieces, (unsigned)Place::count(b));
+}
+
+int comet_attn::launch_values(comet_ctx* ctx, const char* what, ProductParams& p, void* ws, size_t ws_bytes) {
+    const size_t need = values_workspace_bytes((int64_t)p.b.n_tok * p.b.n_heads, p.b.ld, p.d);
+    if (need > 0 && (!ws || ws_bytes < need))
+        return comet_fail(ctx, COMET_EWORKSPACE, "%s: needs %zu bytes of workspace", what, need);
+    if (need > 0 && (reinterpret_cast<uintptr_t>(ws) & 255u) != 0)
+        return comet_fail(ctx, COMET_EALIGN, "%s: the workspace must be 256-byte aligned", what);
+    return launch_split(p, [&](int max_q) { return launch_part(ctx, what, p, max_q, ws); });
 }

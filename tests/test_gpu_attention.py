@@ -238,13 +238,13 @@ def test_more_rows_of_weights_than_one_launch_takes(ctx):
 
 @pytest.mark.parametrize("lens,max_q", [([(9, 30), (1, 3), (0, 4), (2, 8)], 4), ([(1, 900), (0, 0), (0, 7), (40, 700), (1, 1), (0, 9)], None),
                                         ([(0, 3), (30, 30)] + [(1, 20 * s) for s in range(20)], None)])
-@pytest.mark.parametrize("heads,kvh", [(4, 2), (40, 1)])
-def test_prompts_among_single_tokens(ctx, lens, max_q, heads, kvh):
-    say("mixed %s heads=%d" % (lens, heads))
-    k = Case(2320 + len(lens) + heads, lens, heads, kvh, ldp=80, gap=2, pad=3, max_q=max_q, spare=20)
+@pytest.mark.parametrize("heads,kvh,d", [(4, 2, 80), (40, 1, 80), (20, 1, 320), (3, 3, 40)])
+def test_prompts_among_single_tokens(ctx, lens, max_q, heads, kvh, d):
+    say("mixed %s heads=%d d=%d" % (lens, heads, d))
+    k = Case(2320 + len(lens) + heads, lens, heads, kvh, ldp=d, gap=2, pad=3, max_q=max_q, spare=20)
     check_weights(ctx, k, 1, 16, True, False)
-    check_scores(ctx, k, 80, 0, 16, True)
-    check_values(ctx, k, 80, 1, 16, True)
+    check_scores(ctx, k, d, 0, 16, True)
+    check_values(ctx, k, d, 1, 16, True)
 
 
 @pytest.mark.parametrize("new", [1, 30])
