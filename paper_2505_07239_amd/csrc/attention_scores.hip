@@ -260,14 +260,19 @@ static int launch_part(comet_ctx* ctx, const char* what, ProductParams& p, int m
     // below.  576 words: 37 tokens of 64 heads over 2037 keys 273 us (32 x 64: 313; resident rows 807), one token of 64 heads of 4
     // sequences of 4000 keys 69 us (64 x 128: 131), of 16 heads 39 us (resident 64).
     // d <= 256: resident rows (192 words, 512 tokens of 32 heads: 115 us, streamed 197; d = 128: 151 and 172).
+    p.tiles = (int)((n_rows + 63) / 64);
+    const int64_t units64 = filled_tiles(p, 64) * b.n_kv_heads;
+    // Resident rows: tiles of 64, of which a compute unit holds one, where there is one for each or the keys make several pieces of
+    // each; else 32, of which it holds two (100 tokens of 32/8 heads of 128: 12 us, with 64 21; 200 tokens of 40 heads 32 and 42;
+    // 64 tokens of 32 heads over 1000 keys 30.5 and 27.5).
+    const bool wide = n_rows > 32 && (units64 > ctx->num_cu || b.kv_cap >= 1024);
     if (blocks > 8) {
-        p.tiles = (int)((n_rows + 63) / 64);
-        const bool large = n_rows > 32 && filled_tiles(p, 64) * b.n_kv_heads * ((b.kv_cap + 127) / 128) >= ctx->num_cu;
+        const bool large = n_rows > 32 && units64 * ((b.kv_cap + 127) / 128) >= ctx->num_cu;
         if (large) { kern = scores_many_kernel<4, 8>; R = 64; W = 8; }
         else { kern = n_rows > 16 ? scores_many_kernel<2, 4> : scores_many_kernel<1, 4>; R = n_rows > 16 ? 32 : 16; W = 4; }
     }
-    else if (n_rows > 32 && blocks <= 2) { kern = scores_kernel<4, 2, 256>; R = 64; W = 4; }
-    else if (n_rows > 32 && blocks <= 4) { kern = scores_kernel<4, 4, 512>; R = 64; W = 8; }
+    else if (wide && blocks <= 2) { kern = scores_kernel<4, 2, 256>; R = 64; W = 4; }
+    else if (wide && blocks <= 4) { kern = scores_kernel<4, 4, 512>; R = 64; W = 8; }
     else if (n_rows > 16 && blocks <= 4) { kern = scores_kernel<2, 4, 256>; R = 32; W = 4; }
     else if (n_rows > 16) { kern = scores_kernel<2, 8, 512>; R = 32; W = 8; }
     else if (blocks <= 4) { kern = scores_kernel<1, 4, 256>; R = 16; W = 4; }

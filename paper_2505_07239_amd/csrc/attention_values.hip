@@ -315,8 +315,17 @@ static int launch_part(comet_ctx* ctx, const char* what, ProductParams& p, int m
         kern = small ? values_few_kernel<1> : values_few_kernel<4>;
         R = 16; cols = small ? 16 : 64; step = 64 * W;
     }
-    else if (p.d <= 64) { kern = n_rows <= 32 ? values_many_kernel<2, 4> : values_many_kernel<4, 4>; R = n_rows <= 32 ? 32 : 64; cols = 64; step = 64; }
-    else { kern = n_rows <= 32 ? values_many_kernel<2, 8> : values_many_kernel<4, 8>; R = n_rows <= 32 ? 32 : 64; cols = 128; step = 64; }
+    // More: tiles of 64 rows, which convert a cached word half as often as tiles of 32; those where tiles of 64 would occupy up to two
+    // thirds of the compute units (512 tokens of 12 heads of 64: 30 us, with 64 43; 100 tokens of 32/8 heads of 128: 15 and 22; 200 tokens
+    // of 40 heads 26 and 33; 4 x 200 of 12 heads of 64, three quarters, 27 and 25).
+    else {
+        cols = p.d <= 64 ? 64 : 128;
+        p.tiles = (int)((n_rows + 63) / 64);
+        R = n_rows <= 32 || filled_tiles(p, 64) * b.n_kv_heads * ((p.d + cols - 1) / cols) * 3 <= 2 * ctx->num_cu ? 32 : 64;
+        if (cols == 64) kern = R == 32 ? values_many_kernel<2, 4> : values_many_kernel<4, 4>;
+        else kern = R == 32 ? values_many_kernel<2, 8> : values_many_kernel<4, 8>;
+        step = 64;
+    }
     p.tiles = (int)((n_rows + R - 1) / R);
     p.groups = (p.d + cols - 1) / cols;
     // Pieces of the keys: what the longest-working compute unit does, in steps of `step` keys, with two steps for the beginning

@@ -247,6 +247,15 @@ def test_prompts_among_single_tokens(ctx, lens, max_q, heads, kvh, d):
     check_values(ctx, k, d, 1, 16, True)
 
 
+@pytest.mark.parametrize("d", [64, 102])
+def test_many_short_prompts(ctx, d):
+    """Row tiles of 64 for every compute unit over short keys."""
+    say("short prompts d=%d" % d)
+    k = Case(2340 + d, [(17 + s % 3, 18 + s % 7) for s in range(96)], 6, 3, ldp=d, pad=1, mask=d == 102)
+    check_scores(ctx, k, d, 1, 16, True)
+    check_values(ctx, k, d, 0, 16, False)
+
+
 @pytest.mark.parametrize("new", [1, 30])
 def test_no_pages(ctx, new):
     """A cache without pages: no row sees anything, the values are what their masks say."""
