@@ -705,7 +705,8 @@ class Context:
 
     def cache_read(self, party, f_pool, x_pool, slots, width=None, out=None):
         """(F[slots], X_i[slots] - party * F[slots]): cached rows as E and A_i of a share product, [n_tok, width].
-        ``width``: words of a slot (default: those of ``out``, or the pools' elements per entry of their first axis)."""
+        ``width``: words of a slot (default: those of ``out``; of pools [n_pages, page_size, n_kv_heads, words] those of all key
+        heads; of other pools the elements per entry of their first axis)."""
         if out is not None and width is None and len(out) == 2:
             r = self._host.cache_read(party, f_pool, x_pool, slots, out[0], out[1])
             if r is not None:
@@ -713,7 +714,7 @@ class Context:
                 return out[0], out[1]
         _words(f_pool, "f_pool"), _words(x_pool, "x_pool"), _ints(slots, "slots")
         if out is None:
-            width = f_pool[0].numel() if width is None else width
+            width = f_pool.shape[2 if f_pool.dim() == 4 else 1:].numel() if width is None else width
             shape = (slots.numel(), width)
             out = tuple(torch.zeros(shape, dtype=torch.int64, device=f_pool.device) for _ in (0, 1))
         e, a_i = out

@@ -1,0 +1,33 @@
+"""Attention over a cache of shares: calls that the documentation allows and that are easily got wrong, word for word
+against the oracle or a closed form."""
+
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+from oracle import attention as oa                    # noqa: E402
+from test_gpu_attention import PATTERN, Case, U, check_scores, check_values, ctx, down, ints, pattern, say, u64, up  # noqa: E402,F401
+
+
+def test_cache_rows_of_paged_pools(ctx):
+    """Without a width, a slot of pools [pages, slots, key heads, words] has the words of its key heads."""
+    say("cache rows of paged pools")
+    pages, page, kvh, words = 3, 16, 2, 10
+    f, x = (u64(3000, 1 + i, pages, page, kvh, words) for i in (0, 1))
+    flat = lambda v: v.reshape(pages * page, kvh * words)
+    slots = np.array([2, 47, -1, 16, 2, 48], dtype=np.int32)
+    none = np.zeros((len(slots), kvh * words), dtype=U)
+    for party in (0, 1):
+        want = oa.cache_read(party, flat(f), flat(x), slots, none, none)
+        got = ctx.cache_read(party, up(f), up(x), up(slots))
+        assert all(np.array_equal(down(g), w) for g, w in zip(got, want))
+        # one key head's pools without their axis, and flat ones, as before
+        for shape in ((pages * page, kvh, words), (pages * page, kvh * words)):
+            got = ctx.cache_read(party, up(f.reshape(shape)), up(x.reshape(shape)), up(slots))
+            assert all(np.array_equal(down(g), w) for g, w in zip(got, want))
+        got = ctx.cache_read(party, up(f), up(x), up(slots), width=words)      # single key heads' rows
+        want = oa.cache_read(party, f.reshape(-1, words), x.reshape(-1, words), slots, none[:, :words], none[:, :words])
+        assert all(np.array_equal(down(g), w) for g, w in zip(got, want))
