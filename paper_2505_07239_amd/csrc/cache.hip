@@ -164,7 +164,7 @@ int check_rows(comet_ctx* ctx, const char* what, int party, const void* const (&
     if (n_tok < 0 || width < 0 || n_slots < 0) return comet_fail(ctx, COMET_EINVAL, "%s: bad size", what);
     if (n_tok > COMET_DIM_MAX || width > COMET_DIM_MAX || n_slots > 0x7fffffffll)
         return comet_fail(ctx, COMET_ECAP, "%s: n_tok and width must stay below 2^24, n_slots below 2^31", what);
-    if (n_tok == 0 || width == 0) return COMET_OK;
+    if (n_tok == 0 || width == 0 || n_slots == 0) return COMET_OK;
     if (!slots) return comet_fail(ctx, COMET_EINVAL, "%s: null pointer", what);
     for (const void* q : ptrs) {
         if (!q) return comet_fail(ctx, COMET_EINVAL, "%s: null pointer", what);
@@ -182,7 +182,7 @@ int comet_cache_write(comet_ctx* ctx, int party, const uint64_t* d_0, const uint
     const char* what = "comet_cache_write";
     COMET_CHECK_CTX(ctx);
     const int rc = check_rows(ctx, what, party, {d_0, d_1, b_i, f_pool, x_pool}, slots, n_tok, width, n_slots);
-    if (rc != COMET_OK || n_tok == 0 || width == 0) return rc;
+    if (rc != COMET_OK || n_tok == 0 || width == 0 || n_slots == 0) return rc;
     comet_device_guard guard(ctx);
     if (!guard.ok) return comet_fail(ctx, COMET_EDEVICE, "%s: cannot select device", what);
     const bool vec = (width & 1) == 0;
@@ -200,7 +200,7 @@ int comet_cache_read(comet_ctx* ctx, int party, const uint64_t* f_pool, const ui
     const char* what = "comet_cache_read";
     COMET_CHECK_CTX(ctx);
     const int rc = check_rows(ctx, what, party, {f_pool, x_pool, e, a_i, e}, slots, n_tok, width, n_slots);
-    if (rc != COMET_OK || n_tok == 0 || width == 0) return rc;
+    if (rc != COMET_OK || n_tok == 0 || width == 0 || n_slots == 0) return rc;
     comet_device_guard guard(ctx);
     if (!guard.ok) return comet_fail(ctx, COMET_EDEVICE, "%s: cannot select device", what);
     const bool vec = (width & 1) == 0;

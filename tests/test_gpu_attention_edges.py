@@ -31,3 +31,16 @@ def test_cache_rows_of_paged_pools(ctx):
         got = ctx.cache_read(party, up(f), up(x), up(slots), width=words)      # single key heads' rows
         want = oa.cache_read(party, f.reshape(-1, words), x.reshape(-1, words), slots, none[:, :words], none[:, :words])
         assert all(np.array_equal(down(g), w) for g, w in zip(got, want))
+
+
+@pytest.mark.parametrize("shape", [(0, 8), (0, 16, 2, 4)])
+def test_pools_without_slots(ctx, shape):
+    """Every slot is outside pools that have none: nothing is written, and what is read stays as it was."""
+    say("no slots %s" % (shape,))
+    pool = torch.zeros(shape, dtype=torch.int64, device="cuda")
+    rows, slots = u64(3010, 1, 2, 8), ints([0, 5])
+    ctx.cache_write(1, up(rows), up(rows), up(rows), slots, pool, pool.clone())
+    out = (up(pattern(2, 8)), up(pattern(2, 8)))
+    ctx.cache_read(1, pool, pool, slots, out=out)
+    assert all(np.array_equal(down(o), pattern(2, 8)) for o in out)
+    assert not any(down(o).any() for o in ctx.cache_read(0, pool, pool, slots))
