@@ -233,6 +233,7 @@ class KVBatch:
 
     def __init__(self, n_tok, n_heads, n_kv_heads, q_start, kv_len, block_table, page_size, max_q, causal=True,
                  head_mask=None):
+        _fits(n_tok, n_heads, n_kv_heads, page_size, max_q)
         for t, what in ((q_start, "q_start"), (kv_len, "kv_len"), (block_table, "block_table")):
             _ints(t, what)
         n_seq = kv_len.numel()
@@ -250,6 +251,13 @@ class KVBatch:
         self.struct = _Batch(n_seq, n_tok, n_heads, n_kv_heads, page_size, block_table.shape[1], max_q,
                              CAUSAL if causal else 0, *[_ptr(t) for t in (q_start, kv_len, block_table, head_mask)])
         self.ref, self.address = ctypes.byref(self.struct), ctypes.addressof(self.struct)
+
+
+def _fits(*numbers):
+    """Integers that the library takes as 32 bits (ctypes would cut them to those)."""
+    for v in numbers:
+        if not -2 ** 31 <= v < 2 ** 31:
+            raise ValueError("%d does not fit 32 bits" % v)
 
 
 def _ints(t: torch.Tensor, what: str) -> torch.Tensor:
@@ -694,6 +702,7 @@ class Context:
         if r is not None:
             self._made(r)
             return
+        _fits(party)
         _words(d_0, "d_0"), _words(d_1, "d_1"), _words(b_i, "b_i"), _words(f_pool, "f_pool"), _words(x_pool, "x_pool")
         n_tok, width, n_slots = self._rows(slots, d_0, f_pool, x_pool)
         if d_1.shape != d_0.shape or b_i.shape != d_0.shape:
@@ -712,6 +721,7 @@ class Context:
             if r is not None:
                 self._made(r)
                 return out[0], out[1]
+        _fits(party)
         _words(f_pool, "f_pool"), _words(x_pool, "x_pool"), _ints(slots, "slots")
         if out is None:
             width = f_pool.shape[2 if f_pool.dim() == 4 else 1:].numel() if width is None else width
@@ -748,6 +758,7 @@ class Context:
             r = self._host.rotate(party, x_i, positions, cos, sin, n_heads, shift, frac_bits, m_i, interleaved, out)
             if r is not None:
                 return self._made(r)
+        _fits(party, n_heads, shift, frac_bits)
         if x_i.dtype != torch.int64 or not x_i.is_cuda or x_i.dim() != 2 or (x_i.shape[1] > 1 and x_i.stride(1) != 1):
             raise TypeError("x_i must be a 2-D int64 tensor on the GPU with contiguous rows")
         _words(cos, "cos"), _words(sin, "sin"), _ints(positions, "positions")
@@ -773,6 +784,7 @@ class Context:
             r = self._host.product(op == OP_SCORES, party, batch.address, e, a_i, f_pool, x_pool, c_i, frac_bits, m_i, out)
             if r is not None:
                 return self._made(r)
+        _fits(party, frac_bits)
         for t, what in ((e, "E"), (a_i, "A_i"), (f_pool, "f_pool"), (x_pool, "x_pool"), (c_i, "C_i")):
             _words(t, what)
         if e.dim() != 3 or c_i.dim() != 3 or f_pool.dim() != 4:
@@ -818,6 +830,7 @@ class Context:
             if r is not None:
                 self._made(r)
                 return out[0], out[1]
+        _fits(party, frac_bits)
         for t, what in ((d_0, "d_0"), (r_i, "r_i"), (r2_i, "r2_i")):
             _words(t, what)
         if d_0.dim() != 3:

@@ -44,3 +44,30 @@ def test_pools_without_slots(ctx, shape):
     ctx.cache_read(1, pool, pool, slots, out=out)
     assert all(np.array_equal(down(o), pattern(2, 8)) for o in out)
     assert not any(down(o).any() for o in ctx.cache_read(0, pool, pool, slots))
+
+
+def test_numbers_beyond_32_bits_are_refused(ctx):
+    """Not cut to their low 32 bits: a bound of 2^32 tokens would read as none, 2^32 + 16 as 16."""
+    say("numbers beyond 32 bits")
+    import paper_2505_07239_amd as comet
+    k = Case(3020, [(2, 20)], 4, 2, ldp=8)
+    q, kv, table = k.dev["q"], k.dev["kv"], k.dev["table"]
+    sizes = dict(n_tok=k.t, n_heads=4, n_kv_heads=2, page_size=16, max_q=2)
+    for name in sizes:
+        for far in (2 ** 32, -2 ** 32, 2 ** 31, 2 ** 32 + sizes[name]):
+            with pytest.raises(ValueError):
+                comet.KVBatch(q_start=q, kv_len=kv, block_table=table, **dict(sizes, **{name: far}))
+    e, c, z = up(k.words(1, 8)), up(k.words(2, k.ld)), up(k.words(3, 8))
+    f, x = up(k.f), up(k.x)
+    rows, slots, cos = up(u64(3021, 1, 2, 8)), ints([0, 1]), up(u64(3021, 2, 5, 2))
+    pools = up(u64(3021, 3, 4, 8)), up(u64(3021, 4, 4, 8))
+    far = 2 ** 32
+    calls = [lambda: ctx.attention_scores(far, k.batch, e, e, f, x, c), lambda: ctx.attention_scores(0, k.batch, e, e, f, x, c, far + 16),
+             lambda: ctx.attention_values(far + 1, k.batch, c, c, f, x, z), lambda: ctx.attention_values(0, k.batch, c, c, f, x, z, far),
+             lambda: ctx.attention_weights(far, k.batch, c, None, c, c, 5), lambda: ctx.attention_weights(0, k.batch, c, None, c, c, 5, far),
+             lambda: ctx.cache_write(far, rows, rows, rows, slots, *pools), lambda: ctx.cache_read(far, *pools, slots),
+             lambda: ctx.rotate_share(far, rows, slots, cos, cos, 2), lambda: ctx.rotate_share(0, rows, slots, cos, cos, 2, far),
+             lambda: ctx.rotate_share(0, rows, slots, cos, cos, 2, 0, far)]
+    for call in calls:
+        with pytest.raises(ValueError):
+            call()
