@@ -474,7 +474,7 @@ int comet_attention_scores(comet_ctx* ctx, int party, const comet_kv_batch* batc
  *     w_i = t(r2_i + 2 u r_i + party * u^2 by frac_bits),      out = w_i - m_i,      sums(row) = sum_j w_i.
  * m_i (NULL: none) is the mask under which the weights are sent on.  d_0 .. m_i, out: n_tok x n_heads x ld; sums:
  * n_tok x n_heads words, 0 for a row that sees nothing.  out may be any of the inputs.  Of batch only lengths, heads and
- * flags are used; page_size and max_pages bound kv_len as above. */
+ * flags are used; page_size and max_pages bound kv_len as above, block_table may be NULL. */
 int comet_attention_weights(comet_ctx* ctx, int party, const comet_kv_batch* batch, int64_t ld,
                             int frac_bits, uint64_t bias, const uint64_t* d_0, const uint64_t* d_1,
                             const uint64_t* r_i, const uint64_t* r2_i, const uint64_t* m_i,

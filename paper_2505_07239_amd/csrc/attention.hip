@@ -82,8 +82,9 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void weights_kernel(WeightParams
     if (live && lane == 0) p.sums[row] = sum;
 }
 
-// Checks of a batch; fills the device view.  COMET_OK with n_tok == 0 or n_seq == 0 means: nothing to do.
-int make_batch(comet_ctx* ctx, const char* what, const comet_kv_batch* in, int64_t n_pages, int64_t ld, Batch* b) {
+// Checks of a batch; fills the device view.  COMET_OK with n_tok == 0 or n_seq == 0 means: nothing to do.  paged: the call
+// looks up pages.
+int make_batch(comet_ctx* ctx, const char* what, const comet_kv_batch* in, int64_t n_pages, int64_t ld, bool paged, Batch* b) {
     if (!in) return comet_fail(ctx, COMET_EINVAL, "%s: null batch", what);
     if (in->n_seq < 0 || in->n_tok < 0 || in->n_heads < 1 || in->n_kv_heads < 1 || in->n_heads % in->n_kv_heads != 0 ||
         in->max_q < 0 || in->max_pages < 0 || in->page_size < 16 || in->page_size % 16 != 0 || (in->flags & ~COMET_CAUSAL) != 0)
@@ -93,7 +94,7 @@ int make_batch(comet_ctx* ctx, const char* what, const comet_kv_batch* in, int64
         (int64_t)in->n_tok * in->n_heads > 0x7fffffffll || (int64_t)in->n_seq * in->max_q > COMET_DIM_MAX ||
         (int64_t)in->n_seq * in->n_kv_heads > COMET_DIM_MAX)
         return comet_fail(ctx, COMET_ECAP, "%s: ld, n_seq * max_q and n_seq * n_kv_heads must stay below 2^24, rows and slots below 2^31", what);
-    if (in->n_seq > 0 && in->n_tok > 0 && (!in->q_start || !in->kv_len || (in->max_pages > 0 && !in->block_table)))
+    if (in->n_seq > 0 && in->n_tok > 0 && (!in->q_start || !in->kv_len || (paged && in->max_pages > 0 && !in->block_table)))
         return comet_fail(ctx, COMET_EINVAL, "%s: null pointer in the batch", what);
     b->n_seq = in->n_seq; b->n_tok = in->n_tok; b->n_heads = in->n_heads; b->n_kv_heads = in->n_kv_heads;
     b->group = in->n_heads / in->n_kv_heads;
@@ -112,7 +113,7 @@ int make_product(comet_ctx* ctx, const char* what, int party, const comet_kv_bat
                  const uint64_t* x_pool, const uint64_t* C_i, const uint64_t* M_i, uint64_t* Z_i, ProductParams* p) {
     if ((party != 0 && party != 1) || frac_bits < 0 || frac_bits > 62)
         return comet_fail(ctx, COMET_EINVAL, "%s: party must be 0 or 1, 0 <= frac_bits <= 62", what);
-    const int rc = make_batch(ctx, what, batch, n_pages, ld, &p->b);
+    const int rc = make_batch(ctx, what, batch, n_pages, ld, true, &p->b);
     if (rc != COMET_OK) return rc;
     if (d < 1 || (d & 1) || (ldp & 1) || ldp < d) return comet_fail(ctx, COMET_EINVAL, "%s: d and ldp must be even, 1 <= d <= ldp", what);
     if (d > MAX_D || (int64_t)p->b.n_kv_heads * ldp > COMET_DIM_MAX)
@@ -183,7 +184,7 @@ int comet_attention_weights(comet_ctx* ctx, int party, const comet_kv_batch* bat
     if ((party != 0 && party != 1) || frac_bits < 0 || frac_bits > 62)
         return comet_fail(ctx, COMET_EINVAL, "%s: party must be 0 or 1, 0 <= frac_bits <= 62", what);
     WeightParams p;
-    const int rc = make_batch(ctx, what, batch, 1, ld, &p.b);
+    const int rc = make_batch(ctx, what, batch, 1, ld, false, &p.b);
     if (rc != COMET_OK) return rc;
     const Batch& b = p.b;
     if (b.n_tok == 0 || b.n_seq == 0 || b.max_q == 0) return COMET_OK;

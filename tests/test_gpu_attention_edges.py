@@ -1,6 +1,8 @@
 """Attention over a cache of shares: calls that the documentation allows and that are easily got wrong, word for word
 against the oracle or a closed form."""
 
+import ctypes
+
 import numpy as np
 import pytest
 
@@ -71,3 +73,22 @@ def test_numbers_beyond_32_bits_are_refused(ctx):
     for call in calls:
         with pytest.raises(ValueError):
             call()
+
+
+def test_weights_take_a_batch_without_a_page_table(ctx):
+    """Of the batch the weights use lengths, heads and flags only."""
+    say("weights without pages")
+    k = Case(3030, [(2, 20), (1, 5)], 4, 2, mask=True)
+    d_0, r, r2 = (up(k.words(i, k.ld)) for i in (1, 2, 3))
+    outs = [(up(pattern(k.t, 4, k.ld)), up(pattern(k.t, 4))) for _ in (0, 1)]
+    ctx.attention_weights(1, k.batch, d_0, None, r, r2, 7, 16, out=outs[0])
+    bare = type(k.batch.struct)()
+    ctypes.pointer(bare)[0] = k.batch.struct
+    bare.block_table = None
+    p = lambda t: t.data_ptr()
+    assert ctx.lib.comet_attention_weights(ctx.h, 1, ctypes.byref(bare), k.ld, 16, 7, p(d_0), None, p(r), p(r2), None, p(outs[1][0]),
+                                           p(outs[1][1])) == 0
+    assert all(np.array_equal(down(a), down(b)) for a, b in zip(*outs))
+    f, e = up(k.f), up(k.words(4, 8))
+    assert ctx.lib.comet_attention_scores(ctx.h, 1, ctypes.byref(bare), 8, 8, len(k.f), k.ld, 16, p(e), p(e), p(f), p(f), p(d_0), None,
+                                          p(outs[1][0]), None, 0) == -1
