@@ -298,7 +298,7 @@ int64_t max_chunks(int64_t m, int64_t ld, int64_t d) {
 }  // namespace
 
 size_t comet_attn::values_workspace_bytes(int64_t m, int64_t ld, int64_t d) {
-    if (m < 0 || ld < 0 || d < 0 || d > MAX_D || ld > COMET_DIM_MAX || m > 0x7fffffffll) return 0;
+    if (m < 0 || ld < 2 || (ld & 1) || d < 1 || (d & 1) || d > MAX_D || ld > COMET_DIM_MAX || m > 0x7fffffffll) return 0;
     const int64_t n = max_chunks(m, ld, d);
     return n < 2 ? 0 : (size_t)n * m * d * 8;
 }
