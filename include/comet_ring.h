@@ -396,7 +396,7 @@ int comet_truncate_share(comet_ctx* ctx, int party, const uint64_t* z, uint64_t*
  *     F[slots[t]] = d_0[t] + d_1[t],     X_i[slots[t]] = b_i[t] + party * F[slots[t]].
  * d_0, d_1, b_i: n_tok x width; f_pool, x_pool: n_slots x width.  A token whose slot is outside the pools
  * (-1: padding) is skipped.  No slot may occur twice in a call (which token it then holds is
- * unspecified, and may differ from word to word).  The pools must not overlap the inputs.
+ * unspecified, and may differ from word to word).  The pools must not overlap the inputs or each other.
  * n_tok, width < 2^24; n_slots < 2^31. */
 int comet_cache_write(comet_ctx* ctx, int party, const uint64_t* d_0, const uint64_t* d_1,
                       const uint64_t* b_i, const int32_t* slots, int64_t n_tok, int64_t width,
@@ -406,7 +406,7 @@ int comet_cache_write(comet_ctx* ctx, int party, const uint64_t* d_0, const uint
  * comet_somm_share, a row that moves to another cache):
  *     e[t] = F[slots[t]],     a_i[t] = X_i[slots[t]] - party * F[slots[t]].
  * e, a_i: n_tok x width.  The rows of a token whose slot is outside the pools are left as they were; a slot may
- * occur any number of times.  The outputs must not overlap the pools.  Limits as for comet_cache_write. */
+ * occur any number of times.  The outputs must not overlap the pools or each other.  Limits as for comet_cache_write. */
 int comet_cache_read(comet_ctx* ctx, int party, const uint64_t* f_pool, const uint64_t* x_pool,
                      const int32_t* slots, int64_t n_tok, int64_t width, int64_t n_slots, uint64_t* e,
                      uint64_t* a_i);
@@ -473,7 +473,8 @@ int comet_attention_scores(comet_ctx* ctx, int party, const comet_kv_batch* batc
  * with u = d_0 + d_1 + bias:
  *     w_i = t(r2_i + 2 u r_i + party * u^2 by frac_bits),      out = w_i - m_i,      sums(row) = sum_j w_i.
  * m_i (NULL: none) is the mask under which the weights are sent on.  d_0 .. m_i, out: n_tok x n_heads x ld; sums:
- * n_tok x n_heads words, 0 for a row that sees nothing.  out may be any of the inputs.  Of batch only lengths, heads and
+ * n_tok x n_heads words, 0 for a row that sees nothing.  out may be any of the inputs, sums
+ * none of the others.  Of batch only lengths, heads and
  * flags are used; page_size and max_pages bound kv_len as above, block_table may be NULL. */
 int comet_attention_weights(comet_ctx* ctx, int party, const comet_kv_batch* batch, int64_t ld,
                             int frac_bits, uint64_t bias, const uint64_t* d_0, const uint64_t* d_1,

@@ -128,6 +128,8 @@ int make_product(comet_ctx* ctx, const char* what, int party, const comet_kv_bat
         if (!comet_aligned16(q)) return comet_fail(ctx, COMET_EALIGN, "%s: operands must be 16-byte aligned", what);
     }
     if (M_i && !comet_aligned16(M_i)) return comet_fail(ctx, COMET_EALIGN, "%s: operands must be 16-byte aligned", what);
+    if (Z_i == E || Z_i == A_i || Z_i == f_pool || Z_i == x_pool)
+        return comet_fail(ctx, COMET_EINVAL, "%s: Z_i may be C_i or M_i, no other operand", what);
     p->party = party; p->d = d; p->ldp = ldp; p->frac = frac_bits;
     p->E = (const u64*)E; p->A = (const u64*)A_i; p->F = (const u64*)f_pool; p->X = (const u64*)x_pool;
     p->C = (const u64*)C_i; p->M = (const u64*)M_i; p->Z = (u64*)Z_i;
@@ -194,6 +196,7 @@ int comet_attention_weights(comet_ctx* ctx, int party, const comet_kv_batch* bat
     const void* all[] = {d_0, d_1, r_i, r2_i, m_i, out, sums};
     for (const void* q : all)
         if (q && !comet_aligned16(q)) return comet_fail(ctx, COMET_EALIGN, "%s: operands must be 16-byte aligned", what);
+    if (out == sums) return comet_fail(ctx, COMET_EINVAL, "%s: out and sums must not be one buffer", what);
     comet_device_guard guard(ctx);
     if (!guard.ok) return comet_fail(ctx, COMET_EDEVICE, "%s: cannot select device", what);
     p.party = party; p.frac = frac_bits; p.bias = bias;

@@ -183,6 +183,7 @@ int comet_cache_write(comet_ctx* ctx, int party, const uint64_t* d_0, const uint
     COMET_CHECK_CTX(ctx);
     const int rc = check_rows(ctx, what, party, {d_0, d_1, b_i, f_pool, x_pool}, slots, n_tok, width, n_slots);
     if (rc != COMET_OK || n_tok == 0 || width == 0 || n_slots == 0) return rc;
+    if (f_pool == x_pool) return comet_fail(ctx, COMET_EINVAL, "%s: the pools must not be one buffer", what);
     comet_device_guard guard(ctx);
     if (!guard.ok) return comet_fail(ctx, COMET_EDEVICE, "%s: cannot select device", what);
     const bool vec = (width & 1) == 0;
@@ -201,6 +202,7 @@ int comet_cache_read(comet_ctx* ctx, int party, const uint64_t* f_pool, const ui
     COMET_CHECK_CTX(ctx);
     const int rc = check_rows(ctx, what, party, {f_pool, x_pool, e, a_i, e}, slots, n_tok, width, n_slots);
     if (rc != COMET_OK || n_tok == 0 || width == 0 || n_slots == 0) return rc;
+    if (e == a_i) return comet_fail(ctx, COMET_EINVAL, "%s: e and a_i must not be one buffer", what);
     comet_device_guard guard(ctx);
     if (!guard.ok) return comet_fail(ctx, COMET_EDEVICE, "%s: cannot select device", what);
     const bool vec = (width & 1) == 0;

@@ -92,3 +92,22 @@ def test_weights_take_a_batch_without_a_page_table(ctx):
     f, e = up(k.f), up(k.words(4, 8))
     assert ctx.lib.comet_attention_scores(ctx.h, 1, ctypes.byref(bare), 8, 8, len(k.f), k.ld, 16, p(e), p(e), p(f), p(f), p(d_0), None,
                                           p(outs[1][0]), None, 0) == -1
+
+
+def test_results_over_operands_or_each_other_are_refused(ctx):
+    """Where every order of reads and writes would be wrong."""
+    say("results in one buffer")
+    import paper_2505_07239_amd as comet
+    k = Case(3040, [(2, 20)], 4, 2, ldp=32)
+    assert k.ld == 32
+    rows, pool, slots = up(u64(3041, 1, 2, 8)), up(u64(3041, 2, 4, 8)), ints([0, 1])
+    c, e, a, f, x = up(k.words(1, 32)), up(k.words(2, 32)), up(k.words(3, 32)), up(k.f), up(k.x)
+    calls = [lambda: ctx.cache_write(0, rows, rows, rows, slots, pool, pool),
+             lambda: ctx.cache_read(0, pool, pool.clone(), slots, out=(rows, rows)),
+             lambda: ctx.attention_weights(0, k.batch, c, None, c, c, 5, out=(c, c.view(-1)[:k.t * 4].view(k.t, 4)))]
+    for call in (ctx.attention_scores, ctx.attention_values):
+        calls += [lambda call=call, z=z: call(0, k.batch, e, a, f, x, c, 16, out=z) for z in (e, a)]
+    for call in calls:
+        with pytest.raises(comet.CometError) as err:
+            call()
+        assert err.value.code == -1
