@@ -82,14 +82,11 @@ __global__ __launch_bounds__(NT, RF == 1 ? 4 : 2) void scores_kernel(ProductPara
     __shared__ __align__(16) unsigned char rows[KT * R * 512];
     __shared__ RowTile<R> tile;
     const Batch& b = p.b;
-    const Unit unit(b, p.tiles, p.chunks, p.parts);
+    const Unit unit(p, R);
     if (!unit.live) return;
     const Sequence sq(b, unit.s);
-    if (!p.takes(sq)) return;
-    const int kvh = unit.kvh;
-    const int rt = p.tiles - 1 - unit.inner;       // (the rows that see most come first)
-    const int r0 = rt * R;
-    if (r0 >= sq.nq * b.group) return;
+    if (!p.takes(sq) || (int64_t)unit.tile * R >= sq.rows(b)) return;
+    const int kvh = unit.kvh, r0 = unit.tile * R;
     const int first = unit.chunk * p.chunk;
     if (first >= sq.kv) return;
     tile.fill(b, sq, kvh, r0);
@@ -202,13 +199,11 @@ __global__ __launch_bounds__(64 * W) void scores_many_kernel(ProductParams p) {
     __shared__ __align__(16) unsigned char stage[4 * HALF];
     __shared__ RowTile<R> tile;
     const Batch& b = p.b;
-    const Unit unit(b, p.tiles, p.chunks, p.parts);
+    const Unit unit(p, R);
     if (!unit.live) return;
     const Sequence sq(b, unit.s);
-    if (!p.takes(sq)) return;
-    const int r0 = (p.tiles - 1 - unit.inner) * R;
-    if (r0 >= sq.nq * b.group) return;
-    tile.fill(b, sq, unit.kvh, r0);
+    if (!p.takes(sq) || (int64_t)unit.tile * R >= sq.rows(b)) return;
+    tile.fill(b, sq, unit.kvh, unit.tile * R);
     __syncthreads();
     int most, least;
     tile.span(most, least);
@@ -289,9 +284,7 @@ static int launch_part(comet_ctx* ctx, const char* what, ProductParams& p, int m
     if (chunks < 1) chunks = 1;
     p.chunk = (int)(((b.kv_cap + chunks - 1) / chunks + 16 * W - 1) / (16 * W) * (16 * W));
     p.chunks = (b.kv_cap + p.chunk - 1) / p.chunk;
-    p.parts = Unit::parts(b, p.chunks, p.split < 0);
-    const int64_t grid = Unit::grid(b, p.tiles, p.chunks, p.parts);
-    return launch_all(ctx, what, kern, grid, 64 * W, p);
+    return launch_all(ctx, what, kern, Unit::grid(p, R), 64 * W, p);
 }
 
 int comet_attn::launch_scores(comet_ctx* ctx, const char* what, ProductParams& p) {

@@ -32,7 +32,7 @@ struct ProductParams {
     const u64* M;
     u64* Z;
     u64* part;           // partial sums [split][row][d] of the values, null when the keys are not split
-    int tiles;           // row tiles of one key head (host bound)
+    int tiles;           // row tiles of one key head (host bound): of a sequence, or, with split < 0, of the batch (tiles_before)
     int groups;          // column groups of the values
     int chunks, chunk;   // pieces the keys are cut into, keys of a piece
     int parts;           // XCDs that share the units of a piece
@@ -44,8 +44,8 @@ struct ProductParams {
 // One prompt among sequences of a single token each: planned together, the single tokens would get tiles of 64 rows, mostly empty,
 // and long pieces of keys.  So where less than half of the places for tokens can be taken, the sequences whose rows fit a
 // small tile (or a single token) have a launch of their own, planned for them.  One prompt of 512 tokens and 31 sequences of 8000
-// keys, 32 query and 8 key heads of 128 words: scores 2660 us together, 802 apart (floor 680), values 2800
-// and 656.
+// down to 6890 keys, 32 query and 8 key heads of 128 words: scores 2660 us together, 789 apart (floor 680), values 2800
+// and 639 (floor 674 at the rate of a copy; reading alone is faster).
 template <class Launch>
 int launch_split(ProductParams& p, Launch launch) {
     const Batch& b = p.b;
@@ -57,6 +57,14 @@ int launch_split(ProductParams& p, Launch launch) {
     if (rc != COMET_OK) return rc;
     p.split = (signed char)-few;
     return launch(b.max_q);
+}
+// The prompts of a split batch have their row tiles numbered along its tokens, so that a launch has as many as there can be, whatever
+// the number of sequences that might have been prompts: the tiles of a sequence that begins at token q have the numbers from
+// tiles_before(q) on.  A prompt of n > -split tokens ends before the numbers of the next one, as
+// floor((q + n) g / R) - floor(q g / R) + 1 >= ceil(n g / R).  (A prompt of 1024 tokens of 128 heads over one row of 576 words among
+// 255 single tokens, score rows of 4096 words: scores 8.6 ms, values 3.4; with a prompt's tiles for every sequence 50.4 and 11.5.)
+__host__ __device__ inline int tiles_before(const Batch& b, int few, int R, int q) {
+    return (int)((int64_t)q * b.group / R) + q / (few + 1);
 }
 // Row tiles of one key head that a launch may find rows for, over all sequences.
 inline int64_t filled_tiles(const ProductParams& p, int R) {
@@ -97,27 +105,44 @@ __device__ __forceinline__ u64 word_of(const v4i (&acc)[8], int e) {
 // The work of a workgroup: a piece of the keys (chunk) of a (sequence, key head), and which of the `inner` units that read
 // the same cached rows it is.  Those follow each other on one of the eight XCDs, to which workgroups are dealt in turn; where
 // there are few pieces, a piece's units are dealt to several XCDs (parts), so that all have the same number.
+// With split < 0 the tiles of all sequences are one row of units.
 struct Unit {
-    int s, kvh, chunk, inner;
+    int s, kvh, chunk, tile, cg;   // tile: of the sequence, those whose rows see most first; cg: column group
     bool live;
-    __device__ __forceinline__ Unit(const Batch& b, int n_inner, int chunks, int parts) {
-        const unsigned per = ((unsigned)n_inner + parts - 1) / (unsigned)parts;
+    __device__ __forceinline__ Unit(const ProductParams& p, int R) {
+        const Batch& b = p.b;
+        const unsigned n_inner = (unsigned)(p.tiles * p.groups), chunks = (unsigned)p.chunks, parts = (unsigned)p.parts;
+        const unsigned per = (n_inner + parts - 1) / parts;
         const unsigned block = block_number(), q = block >> 3, group = (q / per) * 8 + (block & 7);
-        const unsigned piece = group / (unsigned)parts, pair = piece / (unsigned)chunks;
-        inner = (int)(q % per * (unsigned)parts + group % (unsigned)parts);
-        chunk = (int)(piece % (unsigned)chunks);
-        live = pair < (unsigned)(b.n_seq * b.n_kv_heads) && inner < n_inner;
+        const unsigned piece = group / parts, pair = piece / chunks, inner = q % per * parts + group % parts;
+        chunk = (int)(piece % chunks);
+        live = pair < (unsigned)pairs(p) && inner < n_inner;
         s = (int)(pair / (unsigned)b.n_kv_heads);
         kvh = (int)(pair % (unsigned)b.n_kv_heads);
+        tile = p.tiles - 1 - (int)(inner / (unsigned)p.groups);
+        cg = (int)(inner % (unsigned)p.groups);
+        // (expected rare: otherwise the allocator takes the search for as hot as the main loops, and spills registers in those)
+        if (__builtin_expect(p.split < 0 && live, 0)) find(b, -p.split, R);
     }
-    // one_seq: most of the work may be one sequence's, whose pieces alone have to occupy all XCDs.
-    static int parts(const Batch& b, int64_t chunks, bool one_seq) {
-        const int64_t pieces = (one_seq ? 1 : (int64_t)b.n_seq) * b.n_kv_heads * chunks;
-        if (pieces >= 64) return 1;
-        return pieces % 8 == 0 ? 1 : pieces % 4 == 0 ? 2 : pieces % 2 == 0 ? 4 : 8;
+    // The sequence of tile number `tile`: the last whose tiles begin at or before it.
+    __device__ __forceinline__ void find(const Batch& b, int few, int R) {
+        const int number = tile;
+        s = 0;
+        for (int end = b.n_seq; end - s > 1;) {
+            const int mid = s + (end - s) / 2;
+            if (tiles_before(b, few, R, sequence_start(b, mid)) <= number) s = mid;
+            else end = mid;
+        }
+        tile -= tiles_before(b, few, R, sequence_start(b, s));
+        live = tile >= 0;
     }
-    static int64_t grid(const Batch& b, int64_t n_inner, int64_t chunks, int parts) {
-        return ((int64_t)b.n_seq * b.n_kv_heads * chunks * parts + 7) / 8 * 8 * ((n_inner + parts - 1) / parts);
+    static __host__ __device__ int pairs(const ProductParams& p) { return (p.split < 0 ? 1 : p.b.n_seq) * p.b.n_kv_heads; }
+    // Workgroups of a launch whose pieces and tiles of a sequence are set; deals them out.
+    static int64_t grid(ProductParams& p, int R) {
+        if (p.split < 0) p.tiles = tiles_before(p.b, -p.split, R, p.b.n_tok);
+        const int64_t pieces = (int64_t)pairs(p) * p.chunks;
+        p.parts = pieces >= 64 || pieces % 8 == 0 ? 1 : pieces % 4 == 0 ? 2 : pieces % 2 == 0 ? 4 : 8;
+        return (pieces * p.parts + 7) / 8 * 8 * (((int64_t)p.tiles * p.groups + p.parts - 1) / p.parts);
     }
 };
 
@@ -132,7 +157,7 @@ struct RowTile {
         if (threadIdx.x == 0) row0 = (sq.q0 + r0 / b.group) * b.n_heads + kvh * b.group;
         const int r = r0 + (int)threadIdx.x;
         if ((int)threadIdx.x < R) {
-            const int n = (sq.nq < b.max_q ? sq.nq : b.max_q) * b.group;
+            const int n = sq.rows(b);
             const int j = r / b.group, h = kvh * b.group + r - j * b.group;
             row[threadIdx.x] = r < n ? (sq.q0 + j) * b.n_heads + h : -1;
             sees[threadIdx.x] = r < n ? sq.sees(b, j, h) : 0;

@@ -61,13 +61,12 @@ __global__ __launch_bounds__(NT) void values_few_kernel(ProductParams p) {
     __shared__ RowTile<R> tile;
     __shared__ u64 sums[R * COLS];
     const Batch& b = p.b;
-    const Unit unit(b, p.tiles * p.groups, p.chunks, p.parts);
+    const Unit unit(p, R);
     if (!unit.live) return;
-    const int rt = p.tiles - 1 - unit.inner / p.groups;       // (the rows that see most come first)
-    const int cg = unit.inner % p.groups;
+    const int cg = unit.cg;
     const Sequence sq(b, unit.s);
-    if (rt * R >= sq.nq * b.group || !p.takes(sq)) return;
-    tile.fill(b, sq, unit.kvh, rt * R);
+    if (!p.takes(sq) || (int64_t)unit.tile * R >= sq.rows(b)) return;
+    tile.fill(b, sq, unit.kvh, unit.tile * R);
     const int first = unit.chunk * p.chunk;
     find_slots(slots, b, sq, first, first + p.chunk < sq.kv ? first + p.chunk : sq.kv);
     for (int i = threadIdx.x; i < R * COLS; i += NT) sums[i] = 0;
@@ -168,12 +167,11 @@ __global__ __launch_bounds__(NT) void values_many_kernel(ProductParams p) {
     __shared__ __align__(16) int slots[GROUPS16];
     __shared__ RowTile<R> tile;
     const Batch& b = p.b;
-    const Unit unit(b, p.tiles * p.groups, p.chunks, p.parts);
+    const Unit unit(p, R);
     if (!unit.live) return;
-    const int rt = p.tiles - 1 - unit.inner / p.groups;       // (the rows that see most come first)
-    const int cg = unit.inner % p.groups;
+    const int rt = unit.tile, cg = unit.cg;
     const Sequence sq(b, unit.s);
-    if (rt * R >= sq.nq * b.group || !p.takes(sq)) return;
+    if (!p.takes(sq) || (int64_t)rt * R >= sq.rows(b)) return;
     tile.fill(b, sq, unit.kvh, rt * R);
     const int first = unit.chunk * p.chunk;
     find_slots(slots, b, sq, first, first + p.chunk < sq.kv ? first + p.chunk : sq.kv);
@@ -347,8 +345,7 @@ static int launch_part(comet_ctx* ctx, const char* what, ProductParams& p, int m
     if (p.chunk < 64) p.chunk = 64;
     p.chunks = b.kv_cap > 0 ? (b.kv_cap + p.chunk - 1) / p.chunk : 1;
     p.part = p.chunks > 1 ? (u64*)ws : nullptr;
-    p.parts = Unit::parts(b, p.chunks, p.split < 0);
-    const int64_t grid = Unit::grid(b, (int64_t)p.tiles * p.groups, p.chunks, p.parts);
+    const int64_t grid = Unit::grid(p, R);
     const int pieces = (p.d + 255) / 256;
     const int64_t finish = Place::count(b) * b.n_heads * pieces;
     if (finish > 0x7fffffffll) return comet_fail(ctx, COMET_ECAP, "%s: too many rows", what);

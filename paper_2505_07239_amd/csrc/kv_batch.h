@@ -17,21 +17,27 @@ struct Batch {
     const unsigned char* head_mask;
 };
 
+// Where the tokens of sequence s begin (s = n_seq: where the last one's end).
+__device__ __forceinline__ int sequence_start(const Batch& b, int s) {
+    const int q = b.q_start[s];
+    return q < 0 ? 0 : q > b.n_tok ? b.n_tok : q;
+}
+
 // One sequence, everything clamped to what the operands hold.
 struct Sequence {
     int q0, nq, kv;          // first token, tokens, cached rows
     const int* pages;
 
     __device__ __forceinline__ Sequence(const Batch& b, int s) {
-        int lo = b.q_start[s], hi = b.q_start[s + 1];
-        lo = lo < 0 ? 0 : lo > b.n_tok ? b.n_tok : lo;
-        hi = hi < lo ? lo : hi > b.n_tok ? b.n_tok : hi;
-        q0 = lo;
-        nq = hi - lo;
+        const int end = sequence_start(b, s + 1);
+        q0 = sequence_start(b, s);
+        nq = end < q0 ? 0 : end - q0;
         const int n = b.kv_len[s];
         kv = n < 0 ? 0 : n > b.kv_cap ? b.kv_cap : n;
         pages = b.block_table + (size_t)s * b.max_pages;
     }
+    // rows of a key head that are computed
+    __device__ __forceinline__ int rows(const Batch& b) const { return (nq < b.max_q ? nq : b.max_q) * b.group; }
     // keys that head h of the j-th token sees
     __device__ __forceinline__ int sees(const Batch& b, int j, int h) const {
         int v = kv;
@@ -53,7 +59,7 @@ struct Sequence {
 
 // Kernels with rows of their own count places (sequence, j < max_q), or, where less than half of those could be taken, tokens,
 // whose sequence has to be searched for: one long prompt among many sequences must not cost as many workgroups as a batch of
-// such prompts.  (The weights of four prompts of up to 512 tokens: 91 us by places, 93 by tokens.)
+// such prompts (tiles_before: the same for tiles of rows).  (The weights of four prompts of up to 512 tokens: 91 us by places, 93 by tokens.)
 struct Place {
     int s, token;
     __device__ __forceinline__ Place(const Batch& b, unsigned i) {

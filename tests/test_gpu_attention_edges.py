@@ -111,3 +111,62 @@ def test_results_over_operands_or_each_other_are_refused(ctx):
         with pytest.raises(comet.CometError) as err:
             call()
         assert err.value.code == -1
+
+
+def test_a_prompt_bound_for_many_sequences(ctx):
+    """The work of a batch follows its tokens: 16384 sequences of which any could be the one prompt of 1023 tokens of 128 heads
+    over 8320 keys are 2^31 tiles of rows and keys when every sequence gets a prompt's."""
+    say("prompt bound for many sequences")
+    import paper_2505_07239_amd as comet
+    n_seq, max_q, t, heads, page, d, ld = 16384, 1023, 1040, 128, 1664, 258, 8320
+    lens = {3: (5, 40), 9000: (1, 70), 9001: (0, 9), 16383: (3, 2)}
+    new, kv_len = np.zeros(n_seq, dtype=np.int32), np.zeros(n_seq, dtype=np.int32)
+    for s, (n, kv) in lens.items():
+        new[s], kv_len[s] = n, kv
+    q_start = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+    table = (np.arange(n_seq, dtype=np.int32)[:, None] + np.arange(ld // page, dtype=np.int32)) % 3
+    batch = comet.KVBatch(t, heads, 1, ints(q_start), ints(kv_len), ints(table), page, max_q)
+    used, n = int(q_start[-1]), 80
+    rows = list(oa.rows(q_start, kv_len, heads))
+    f, x = (u64(3050, 1 + i, 3, page, 1, d) for i in (0, 1))
+    e, a, c = u64(3050, 3, used, heads, d), u64(3050, 4, used, heads, d), u64(3050, 5, used, heads, n)
+    filled = lambda v: torch.cat([up(v), torch.full((t - used,) + v.shape[1:], PATTERN, dtype=torch.int64, device="cuda")])
+    z = torch.full((t, heads, ld), PATTERN, dtype=torch.int64, device="cuda")
+    z[:used, :, :n] = up(c)
+    ctx.attention_scores(1, batch, filled(e), filled(a), up(f), up(x), z, 16, out=z)
+    assert np.array_equal(down(z[:used, :, :n].contiguous()), oa.scores(1, rows, e, a, f, x, table, c, 16, None, c))
+    assert bool((z[:used, :, n:] == PATTERN).all()) and bool((z[used:] == PATTERN).all())
+
+
+@pytest.mark.parametrize("heads,kvh", [(1, 1), (6, 2), (21, 1), (40, 1)])
+@pytest.mark.parametrize("d", [40, 130, 320])
+def test_where_the_tiles_of_prompts_lie(ctx, heads, kvh, d):
+    """Prompts of every length between, behind and in front of single tokens and empty sequences, tokens before the first
+    sequence and behind the last, more sequences than a wavefront has lanes."""
+    say("tiles of prompts heads=%d kvh=%d d=%d" % (heads, kvh, d))
+    few = max(16 * kvh // heads, 1)
+    lens = [(0, 3), (few + 1, 40), (1, 9), (0, 0), (few + 1, few + 1), (few + 2, 7), (0, 5), (70, 90), (1, 33)]
+    lens += [(s % 2, 2 + s) for s in range(75)] + [(few, 30), (33, 33)] + [(0, 1)] * 60 + [(few + 1, 20), (0, 4)]
+    k = Case(3060 + d + heads, lens, heads, kvh, ldp=d, gap=5, pad=4, mask=d == 40)
+    check_scores(ctx, k, d, 1, 16, True)
+    check_values(ctx, k, d, 0, 16, True)
+    k = Case(3070 + d + heads, [(0, 3)] * 70 + [(67, 67)], heads, kvh, ldp=d, max_q=30)
+    check_scores(ctx, k, d, 0, 0, False)
+    check_values(ctx, k, d, 1, 0, False)
+
+
+def test_token_ranges_that_do_not_ascend(ctx):
+    """What they give is unspecified; every access stays in the operands and the call ends."""
+    say("ranges that do not ascend")
+    k = Case(3080, [(20, 30), (1, 5)] + [(0, 2)] * 70 + [(25, 60)], 4, 2, ldp=64)
+    e, a, c, z = (up(k.words(i, n)) for i, n in ((1, 64), (2, 64), (3, k.ld), (4, 64)))
+    starts = list(k.q_start)
+    for order in (starts[::-1], [k.t] * len(starts), [1 << 30] + starts[1:], [-5, 40, 3] + starts[3:]):
+        k.dev["q"].copy_(ints(order))
+        ctx.attention_scores(1, k.batch, e, a, up(k.f), up(k.x), c, 16)
+        ctx.attention_values(1, k.batch, c, c, up(k.f), up(k.x), z, 16)
+        ctx.attention_weights(1, k.batch, c, None, c, c, 5)
+        torch.cuda.synchronize()
+    k.dev["q"].copy_(ints(starts))
+    check_scores(ctx, k, 64, 1, 16, True)
+    check_values(ctx, k, 64, 1, 16, True)
