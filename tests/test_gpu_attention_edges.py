@@ -170,3 +170,133 @@ def test_token_ranges_that_do_not_ascend(ctx):
     k.dev["q"].copy_(ints(starts))
     check_scores(ctx, k, 64, 1, 16, True)
     check_values(ctx, k, 64, 1, 16, True)
+
+
+DIGITS = [0x7F7F7F7F7F7F7F80, 0x7F7F7F7F7F7F7F7F]      # all eight signed digits -128, all 127
+
+
+@pytest.mark.parametrize("d", [66, 128])
+@pytest.mark.parametrize("kv", [8128, 8129, 16256])
+@pytest.mark.parametrize("value", DIGITS)
+def test_longest_pieces_of_keys(ctx, value, kv, d):
+    """Digits of the largest magnitude in as many keys as one accumulator takes: 64 tokens of 256 heads, a tile of rows for every
+    compute unit, so that cutting the keys further than the planes need does not pay.  Every row is c + 2 kv value^2."""
+    say("longest pieces kv=%d d=%d %x" % (kv, d, value))
+    import paper_2505_07239_amd as comet
+    t, heads, page = 64, 256, 16
+    ld = -(-kv // page) * page
+    batch = comet.KVBatch(t, heads, heads, ints([0, t]), ints([kv]), torch.zeros((1, ld // page), dtype=torch.int32, device="cuda"), page, t,
+                          causal=False)
+    full = lambda *shape: torch.full(shape, value, dtype=torch.int64, device="cuda")
+    w, pool, c = full(t, heads, ld), full(1, page, heads, d), up(u64(3090, 1, t, heads, d))
+    got = ctx.attention_values(1, batch, w, w, pool, pool, c)
+    assert torch.equal(got, c + up(np.array([2 * kv * value * value % 2 ** 64], dtype=np.uint64)))
+
+
+@pytest.mark.parametrize("value", DIGITS)
+@pytest.mark.parametrize("t,heads", [(1, 3), (3, 8), (2, 300)])
+def test_longest_rows_of_keys(ctx, value, t, heads):
+    """The same for scores: rows of 4096 words."""
+    say("longest rows %d x %d" % (t, heads))
+    import paper_2505_07239_amd as comet
+    d, kv, ld = 4096, 130, 144
+    batch = comet.KVBatch(t, heads, 1, ints([0, t]), ints([kv]), torch.zeros((1, 9), dtype=torch.int32, device="cuda"), 16, t, causal=False)
+    full = lambda *shape: torch.full(shape, value, dtype=torch.int64, device="cuda")
+    q, pool, c = full(t, heads, d), full(1, 16, 1, d), up(u64(3091, 1, t, heads, ld))
+    got = ctx.attention_scores(1, batch, q, q, pool, pool, c)
+    want = c + up(np.array([2 * d * value * value % 2 ** 64], dtype=np.uint64))
+    want[:, :, kv:] = 0
+    assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("d,ldp", [(194, 194), (256, 256), (256, 260), (258, 258)])
+@pytest.mark.parametrize("new,heads,kvh", [(1, 4, 1), (1, 16, 1), (5, 8, 1), (1, 40, 1), (20, 6, 1), (70, 2, 2)])
+def test_widths_about_256(ctx, d, ldp, new, heads, kvh):
+    """Where the rows' digits just fill the place they have, and just do not."""
+    say("width %d of %d, %d tokens of %d heads" % (d, ldp, new, heads))
+    k = Case(3100 + d + new + heads, [(new, new + 60), (new, 200)], heads, kvh, ldp=ldp)
+    check_scores(ctx, k, d, 1, 16, True)
+    check_values(ctx, k, d, 0, 16, True)
+
+
+def test_pools_of_more_than_4_gb(ctx):
+    """Slots beyond 2^32 bytes of a pool, written, read and multiplied with."""
+    say("pools of more than 4 GB")
+    import paper_2505_07239_amd as comet
+    page, kvh, d, n_pages = 64, 8, 128, 9000                  # 64 * 8 KB a page: 4.7 GB
+    assert n_pages * page * kvh * d * 8 > 2 ** 32 + 2 ** 28
+    f, x = (torch.zeros((n_pages, page, kvh, d), dtype=torch.int64, device="cuda") for _ in (0, 1))
+    last, first = n_pages - 1, 3
+    kv, heads, new = 100, 16, 3
+    slots = np.array([last * page + j for j in range(64)] + [first * page + j for j in range(36)], dtype=np.int32)
+    d_0, d_1, b = (u64(3110, 1 + i, kv, kvh * d) for i in range(3))
+    ctx.cache_write(1, up(d_0), up(d_1), up(b), up(slots), f, x)
+    fv = d_0 + d_1
+    e, a = ctx.cache_read(1, f, x, up(slots))
+    assert np.array_equal(down(e), fv) and np.array_equal(down(a), b)
+    assert int(f.ne(0).sum()) == kv * kvh * d                 # (no word of these is zero)
+    small = [np.zeros((2, page, kvh, d), dtype=U) for _ in (0, 1)]
+    for p, v in zip(small, (fv, b + fv)):
+        p.reshape(2 * page, kvh * d)[:kv] = v
+    rows, table = list(oa.rows([0, new], [kv], heads)), np.array([[0, 1]])
+    batch = comet.KVBatch(new, heads, kvh, ints([0, new]), ints([kv]), ints([[last, first]]), page, new)
+    e, a, c, z = u64(3111, 1, new, heads, d), u64(3111, 2, new, heads, d), u64(3111, 3, new, heads, 2 * page), u64(3111, 4, new, heads, d)
+    got = ctx.attention_scores(0, batch, up(e), up(a), f, x, up(c), 16)
+    assert np.array_equal(down(got), oa.scores(0, rows, e, a, *small, table, c, 16, None, np.zeros_like(c)))
+    got = ctx.attention_values(0, batch, up(c), up(c), f, x, up(z), 16)
+    assert np.array_equal(down(got), oa.values(0, rows, c, c, *small, table, z, 16, None, np.zeros_like(z)))
+
+
+def test_graph_replayed_with_new_operands_in_place(ctx):
+    """Queries, keys, values, pools, triple parts, pages, tokens of the sequences and active heads all change between replays."""
+    say("graph with new operands")
+    k = Case(3120, [(1, 40), (30, 70), (2, 9)], 4, 2, ldp=80, page=16, mask=True, pad=6, spare=1)
+    d, n = 80, 6
+    host = dict(e=k.words(1, d), a=k.words(2, d), c=k.words(3, k.ld), r=k.words(4, k.ld), r2=k.words(5, k.ld), m=k.words(6, k.ld),
+                z=k.words(7, d), f=k.f, x=k.x)
+    dev = {name: up(v) for name, v in host.items()}
+    slots = ints(np.arange(n))
+
+    def run():
+        s = ctx.attention_scores(1, k.batch, dev["e"], dev["a"], dev["f"], dev["x"], dev["c"], 16, dev["r"])
+        w, sums = ctx.attention_weights(1, k.batch, s, None, dev["r"], dev["r2"], 9, 16, dev["m"])
+        o = ctx.attention_values(1, k.batch, w, dev["m"], dev["f"], dev["x"], dev["z"], 16)
+        return [s, w, sums, o, *ctx.cache_read(1, dev["f"], dev["x"], slots, width=2 * d)]
+
+    def want():
+        rows = list(oa.rows(k.q_start, k.kv_len, 4, True, k.mask))
+        none = lambda v: np.zeros_like(v)
+        s = oa.scores(1, rows, host["e"], host["a"], host["f"], host["x"], k.table, host["c"], 16, host["r"], none(host["c"]))
+        w, sums = oa.weights(1, rows, s, None, host["r"], host["r2"], 9, 16, host["m"], none(s), np.zeros((k.t, 4), dtype=U))
+        o = oa.values(1, rows, w, host["m"], host["f"], host["x"], k.table, host["z"], 16, None, none(host["z"]))
+        flat = lambda v: v.reshape(-1, 2 * d)
+        at = down(slots.long()).astype(np.int64)
+        none = np.zeros((n, 2 * d), dtype=U)
+        return [s, w, sums, o, *oa.cache_read(1, flat(host["f"]), flat(host["x"]), at, none, none)]
+
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        eager = run()
+        assert all(np.array_equal(down(g), w) for g, w in zip(eager, want()))
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            held = run()
+    for turn, lens in enumerate(([(1, 40), (30, 70), (2, 9)], [(0, 3), (1, 8), (30, 96)], [(16, 16), (15, 70), (8, 8)], [(1, 1), (1, 50), (1, 77)])):
+        for i, name in enumerate(host):
+            host[name] = u64(3121 + turn, i, *host[name].shape)
+            dev[name].copy_(up(host[name]))
+        k.q_start = [0] + list(np.cumsum([new for new, _ in lens]))
+        k.kv_len = [kv for _, kv in lens]
+        k.mask = (u64(3125 + turn, 1, k.t, 4) & U(1)).astype(np.uint8)
+        k.table = k.table[::-1].copy()
+        for name, v in (("q", k.q_start), ("kv", k.kv_len), ("table", k.table)):
+            k.dev[name].copy_(ints(v))
+        k.batch.tensors[3].copy_(up(k.mask))
+        slots.copy_(ints(np.arange(n) * (turn + 2)))
+        torch.cuda.synchronize()
+        ctx.open(up(u64(3126, turn, 1000)), up(u64(3127, turn, 1000)))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(np.array_equal(down(h), w) for h, w in zip(held, want()))
