@@ -167,7 +167,7 @@ struct RowTile {
     __device__ __forceinline__ void span(int& most, int& least) const {
         int hi = sees[threadIdx.x % R], lo = hi;
 #pragma unroll
-        for (int n = 1; n < (R & (R - 1) ? 64 : R); n *= 2) {
+        for (int n = 1; n < R; n *= 2) {
             const int a = __shfl_xor(hi, n), c = __shfl_xor(lo, n);
             hi = a > hi ? a : hi;
             lo = c < lo ? c : lo;

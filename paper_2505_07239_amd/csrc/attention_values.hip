@@ -18,7 +18,6 @@
 // values_finish_kernel adds up.
 #include "attention_tile.h"
 
-
 using namespace comet_attn;
 
 namespace {

@@ -392,9 +392,8 @@ PyObject* group(Host* self, PyObject* const* arg, Py_ssize_t nargs) {
 }
 
 // ---------------------------------------------------------------------------
-// the type and the module
+// attention over a cache of shares: results are the caller's, everything is on the context's device
 // ---------------------------------------------------------------------------
-// ---- attention over a cache of shares: results are the caller's, everything is on the context's device ----
 
 const Tensor* here(Host* self, const Tensor* t) { return t && t->get_device() == self->device ? t : nullptr; }
 const Tensor* words_here(Host* self, PyObject* o) { return here(self, words(o)); }
@@ -548,6 +547,9 @@ PyObject* weights(Host* self, PyObject* const* arg, Py_ssize_t nargs) {
     END_HANDLE_TH_ERRORS
 }
 
+// ---------------------------------------------------------------------------
+// the type and the module
+// ---------------------------------------------------------------------------
 PyObject* host_new(PyTypeObject* type, PyObject* args, PyObject*) {
     unsigned long long ctx;
     int device;
