@@ -435,10 +435,11 @@ int comet_rotate_share(comet_ctx* ctx, int party, const uint64_t* x_i, int64_t l
  * SEES the first v(t, h) keys of its sequence: kv_len[s], or with COMET_CAUSAL
  * max(kv_len[s] - n_q + j + 1, 0) for the j-th of n_q new tokens; none when head_mask (n_tok x n_heads bytes, may be
  * NULL) has a zero for it.  An n_tok x n_heads x ld matrix holds a word for every row and key; of its rows
- * only the first v words are ever read or written.  Tokens outside every sequence (padding) are left as they were.
- * What does not fit stays in bounds: q_start is read as ascending within 0 .. n_tok, kv_len as at most
+ * only the first v words count, and only those are written.  All of its words must be readable: whole blocks are
+ * loaded, and what a row does not see is dropped.  Tokens outside every sequence (padding) are left as they were.
+ * What does not fit stays in bounds: q_start is read as at least 0 and at most n_tok, kv_len as at most
  * min(ld, max_pages * page_size), a page id outside 0 .. n_pages - 1 as 0; tokens of a sequence at or beyond the
- * max_q-th are not computed. */
+ * max_q-th are not computed.  Which rows are computed where q_start does not ascend is unspecified. */
 typedef struct comet_kv_batch {
     int32_t n_seq, n_tok;
     int32_t n_heads, n_kv_heads;    /* n_heads a multiple of n_kv_heads */
@@ -458,7 +459,8 @@ enum { COMET_CAUSAL = 1 };
  * none).  E, A_i: n_tok x n_heads x d (opened masked queries, and their mask's share); C_i, M_i, Z_i: n_tok x n_heads x
  * ld; pools: n_pages * page_size slots of n_kv_heads x ldp words.
  * d and ldp even, 1 <= d <= ldp, d <= 4096; n_kv_heads * ldp < 2^24; ld even, 2 <= ld < 2^24; n_tok * n_heads < 2^31;
- * n_pages * page_size < 2^31; n_seq * max_q and n_seq * n_kv_heads < 2^24.
+ * n_pages * page_size < 2^31; n_seq * max_q and n_seq * n_kv_heads < 2^24.  (Workgroups are planned for every sequence
+ * and ld keys: millions of sequences with rows of tens of thousands of words may need 2^31 or more, COMET_ECAP too.)
  * Z_i may be C_i or M_i; it must not overlap anything else.
  * ws: comet_workspace_bytes(COMET_OP_SCORES, n_tok * n_heads, d, ld, 0) bytes (0: none). */
 int comet_attention_scores(comet_ctx* ctx, int party, const comet_kv_batch* batch, int d, int ldp,
