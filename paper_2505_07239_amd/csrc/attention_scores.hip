@@ -11,12 +11,14 @@
 // What bounds them (us of a call; the floor at 5.9 TB/s and 3.9 POP/s):
 //   * few rows, the cache read once: HBM.  16 sequences of up to 8193 keys, 8 key heads of 128 words, 4 rows each: 280 (floor 262,
 //     5.5 TB/s).  Loads past the caches are slower here (374): a load takes half a line, the next one the other half.
-//   * prompts, 4 of up to 512 tokens, 32 heads of 128: 153 (floor 75, matrix units busy 31 %).  By time stamps a workgroup of 64 rows
+//   * prompts, 4 of up to 512 tokens, 32 heads of 128: 153 (floor 75, matrix units busy 30 %).  By time stamps a workgroup of 64 rows
 //     takes 7 us to begin (its row's digits 5), then per tile and pair of wavefronts 10 us of multiplying, in which the matrix units
 //     are busy for nine tenths, and 7 of writing out, in which they are not.  Tried, without gain: 32 and 48 rows, more
 //     workgroups of fewer rows or keys, C and M requested early (registers, or their lines into L2), priorities.
 //   * latent rows, 64 heads of 4 sequences over 576 words: 62 (floor 22): a chain of nine blocks whose loads one wavefront per SIMD
 //     cannot cover; smaller tiles that would add wavefronts split the keys more often (85).
+//   * latent rows, 37 tokens of 64 heads over 2037 keys: 243 to 254 (floor 102): the conversion of both sides, and 36 registers of
+//     scores_many_kernel<4, 8> that do not fit and are reloaded in its loop.
 #include "attention_tile.h"
 
 using namespace comet_attn;
@@ -252,7 +254,7 @@ static int launch_part(comet_ctx* ctx, const char* what, ProductParams& p, int m
     void (*kern)(ProductParams);
     // d > 256: the rows' digits would fill LDS (and 16 rows of them would leave one workgroup on a compute unit): the contraction is
     // streamed, with tiles of 64 x 128 where there is one for every compute unit, smaller ones, of which a compute unit holds several,
-    // below.  576 words: 37 tokens of 64 heads over 2037 keys 273 us (32 x 64: 313; resident rows 807), one token of 64 heads of 4
+    // below.  576 words, when this was settled: 37 tokens of 64 heads over 2037 keys 273 us (32 x 64: 313; resident rows 807), one token of 64 heads of 4
     // sequences of 4000 keys 69 us (64 x 128: 131), of 16 heads 39 us (resident 64).
     // d <= 256: resident rows (192 words, 512 tokens of 32 heads: 115 us, streamed 197; d = 128: 151 and 172).
     p.tiles = (int)((n_rows + 63) / 64);

@@ -12,7 +12,7 @@
 //     weights, which all of them need, are converted once by all threads into one of two LDS stages while the other is
 //     multiplied (sweep_blocks in attention_tile.h).  With at most 64 columns four wavefronts take E X and four A F.
 //     Bound by the matrix units and power: 512 tokens of 32 heads over 4608 keys, 560 us (floor 337 at 3.9 POP/s of random
-//     operands), matrix units busy 59 % of the cycles at 1.87 GHz.  With 48 rows 648, with the two wavefronts of a SIMD in step
+//     operands), matrix units busy 61 % of the cycles at 1.84 GHz.  With 48 rows 648, with the two wavefronts of a SIMD in step
 //     and 64 rows 830; a barrier that waits for memory, or a spilled register in the loop, costs as much.
 // Long sequences with few rows are cut into pieces, whose sums (of words, so that their order changes nothing)
 // values_finish_kernel adds up.
